@@ -88,7 +88,7 @@ typedef struct {
     int32_t norm_topk;    /* 1: renormalise the K selected gates to sum 1 */
     int32_t conf_mode;    /* SPICE_CONF_* */
     float tau;            /* confidence threshold: LoRE iff conf < tau (NaN conf -> exact) */
-    int32_t wfmt;         /* routed experts' weight format: SPICE_WFMT_DTYPE or SPICE_WFMT_MXFP4 */
+    int32_t wfmt;         /* routed experts' weight format: SPICE_WFMT_* */
 } spice_moe_cfg_t;
 
 /* Weight formats of the routed experts (the pool slots and the host copies).
@@ -104,9 +104,20 @@ typedef struct {
  *   2 GiB.  The fetched-expert split (moe_split_plan,
  *   moe_fetch_experts, moe_expert_ffn_fetched) and moe_lore_fit return UNSUPPORTED for it.
  *   With many tokens the expert FFN runs on the prefill GEMMs where d and inter are
- *   multiples of 128 and the pools 16-byte aligned, otherwise on the streaming kernels. */
-enum { SPICE_WFMT_DTYPE = 0, SPICE_WFMT_MXFP4 = 2 };
+ *   multiples of 128 and the pools 16-byte aligned, otherwise on the streaming kernels.
+ * SPICE_WFMT_INT8: 8-bit integers with one scale per output channel, for the routed experts and
+ *   for the shared block.  A [rows][K] matrix is one byte blob: rows*K int8 codes, row-major, then
+ *   rows fp32 scales; element value = scale[row] * code.  A W13 blob holds [2I][d] (2I*d + 8I
+ *   bytes), a W2 blob [d][I] (d*I + 4d bytes); a pool slot is one such blob.  Needs dtype
+ *   SPICE_BF16 (activations, router and LoRE factors stay bf16), d, inter and shared_inter
+ *   multiples of 16, inter and shared_inter at most SPICE_INT8_MAX_K, and 16-byte aligned pools.
+ *   Its expert FFN is moe_expert_ffn_grouped_i8, whose activations are 8-bit too;
+ *   moe_route_bucket(_scored), lore_surrogate_apply, moe_combine, moe_exact_residual_host (which
+ *   keeps its activations in fp32), the cache and moe_spec_update take it, every other call returns
+ *   UNSUPPORTED for it. */
+enum { SPICE_WFMT_DTYPE = 0, SPICE_WFMT_MXFP4 = 2, SPICE_WFMT_INT8 = 3 };
 #define SPICE_MXFP4_MAX_K 4096
+#define SPICE_INT8_MAX_K 131056 /* sums of 128 * 128 stay in 32 bits */
 
 /* Size alignment required: d, inter and shared_inter multiples of 8 (bf16) or 4 (fp32);
  * lore_rank a multiple of 8 (bf16) or 4 (fp32). */
@@ -183,6 +194,61 @@ spice_status_t moe_route_bucket(const spice_moe_cfg_t* cfg, int32_t T, const voi
                                 const spice_host_out_t* host_out, void* ws, size_t ws_bytes,
                                 spice_stream_t stream);
 
+/* How a router's logits choose experts and weigh them (moe_route_bucket_scored). */
+enum { SPICE_SCORE_SOFTMAX = 0, SPICE_SCORE_SIGMOID = 1 };
+typedef struct {
+    int32_t score;             /* SPICE_SCORE_* of the logits, over all N */
+    int32_t n_group;           /* G groups of N/G consecutive experts, at most 64; 1: no groups */
+    int32_t topk_group;        /* groups a token may choose from, 1..G */
+    int32_t group_top;         /* 1 or 2: a group counts as the sum of so many of its largest choice values */
+    float scale;               /* factor on the weights (finite) */
+    const float* balance_bias; /* device [N] fp32, added to the scores for the choice only; or NULL */
+} spice_route_score_t;
+
+/*
+ * Steps 1-2 with another scoring rule: as moe_route_bucket (same outputs, classes, buckets, host
+ * copies and workspace), but per token
+ *   s = softmax(z) over all N, or sigmoid(z) of each;   c = s + balance_bias;
+ *   the topk_group groups with the largest group values are kept (ties -> lower group);
+ *   the K largest c among the kept groups are chosen, in descending order (ties -> lower expert id);
+ *   g = s of the chosen (without the bias), with cfg->norm_topk divided by its sum over the K;
+ *   topk_w = g * scale; the confidence modes GATE and GATE_RENORM read g.
+ * All of it is computed in fp64 from fp64 logits; topk_w is rounded once.  A logit of -inf (through
+ * logit_bias) masks its expert: its score is 0, it counts in no group value, and it is chosen, with
+ * weight 0, only when a token's kept groups have fewer than K others.  Weights whose sum is 0 stay 0.
+ * Logits that are NaN or +inf give valid experts and unspecified weights.
+ *   score   host struct; N must be a multiple of n_group and topk_group * N/n_group at least K
+ *   logits  device [T][N] fp64 out, or NULL: z, as in moe_route_bucket
+ * Errors: as moe_route_bucket, plus INVALID for a bad *score, UNSUPPORTED for n_group above 64.
+ */
+spice_status_t moe_route_bucket_scored(const spice_moe_cfg_t* cfg, const spice_route_score_t* score, int32_t T,
+                                       const void* x, const void* w_gate, const float* logit_bias,
+                                       const int32_t* resident_slot, const float* conf, double* logits,
+                                       int32_t* topk_idx, float* topk_w, uint8_t* slot_class, int32_t* offsets,
+                                       int32_t* perm, int32_t* inv_perm, const spice_host_out_t* host_out,
+                                       void* ws, size_t ws_bytes, spice_stream_t stream);
+
+/*
+ * RMS norm with the residual's addition, in front of a layer's routing and experts:
+ *   s = x + resid;  h = s rounded to the dtype;  y = s * w / sqrt(mean(s^2) + eps);
+ *   q_scale = max |y| / 127;  q = y / q_scale rounded to the nearest integer, ties to even.
+ * s is not rounded before y and q.  The arithmetic is fp64; h, y and q_scale go through fp32.
+ * A row of zeros gives y 0, q 0 and q_scale 0; a row with NaN or infinities in s or s * w gives q 0
+ * and q_scale NaN.
+ *   x, resid  device [T][d] (dtype); resid NULL: s = x
+ *   weight    device [d] (dtype), or NULL: 1
+ *   eps       finite, >= 0
+ *   h_out     device [T][d] (dtype) out, or NULL; it may be x or resid itself
+ *   y_out     device [T][d] (dtype) out, or NULL; it may be x or resid itself
+ *   q_out, q_scale  device [T][d] int8 and [T] fp32 out (both or neither)
+ * At least one of h_out, y_out and q_out.  Rows of buffers 16-byte aligned.  No workspace.
+ * Errors: INVALID for a missing pointer, a bad eps or outputs that overlap an input (without being
+ * it) or each other; UNSUPPORTED for a buffer that is not aligned.
+ */
+spice_status_t moe_rmsnorm_quant(const spice_moe_cfg_t* cfg, int32_t T, const void* x, const void* resid,
+                                 const void* weight, float eps, void* h_out, void* y_out, int8_t* q_out,
+                                 float* q_scale, spice_stream_t stream);
+
 /*
  * Step 3: grouped SwiGLU FFN y = W2 (silu(W1 x) * (W3 x)) (Eq. 6) for every HIT slot,
  * grouped by expert, plus the shared block S(x) (Sec. 2.1, 4.2) for all T tokens.
@@ -226,6 +292,30 @@ spice_status_t moe_expert_ffn_grouped_gated(const spice_moe_cfg_t* cfg, int32_t 
                                             const void* lore_A, const void* lore_B, float* y_slots,
                                             float* y_shared, void* ws, size_t ws_bytes,
                                             spice_stream_t stream);
+
+/*
+ * Step 3 with 8-bit weights and activations (cfg->wfmt SPICE_WFMT_INT8): for every HIT slot, grouped by
+ * expert, and for the shared block on all T tokens
+ *   g = sx * s1 * sum_k q1 qx,  u = sx * s3 * sum_k q3 qx          (int32 sums, exact)
+ *   h = silu(g) u;  sh = max |h| / 127 over the row;  qh = h / sh rounded to the nearest integer
+ *   y = sh * s2 * sum_k q2 qh                                      (int32 sums, exact)
+ * h, the scales and y are fp32.  A row whose x_scale or max |h| is not finite comes out NaN.
+ *   x_q, x_scale  device [T][d] int8 and [T] fp32: the activations, e.g. from moe_rmsnorm_quant
+ *   x             device [T][d] bf16 of the same activations: read by the shared gate and by LoRE;
+ *                 NULL without them
+ *   w13_pool, w2_pool, w13_shared, w2_shared  device blobs (see SPICE_WFMT_INT8)
+ *   w_shared_gate device [d] bf16, or NULL: as in moe_expert_ffn_grouped_gated
+ *   lore_A, lore_B  as in lore_surrogate_apply (whose launches follow when both are given), or NULL
+ *   perm, offsets, resident_slot, y_slots, y_shared, ws  as in moe_expert_ffn_grouped
+ * Errors: as moe_expert_ffn_grouped, plus UNSUPPORTED for another wfmt or unaligned buffers (16 bytes).
+ */
+spice_status_t moe_expert_ffn_grouped_i8(const spice_moe_cfg_t* cfg, int32_t T, const int8_t* x_q,
+                                         const float* x_scale, const void* x, const int32_t* perm,
+                                         const int32_t* offsets, const int32_t* resident_slot,
+                                         const void* w13_pool, const void* w2_pool, const void* w13_shared,
+                                         const void* w2_shared, const void* w_shared_gate, const void* lore_A,
+                                         const void* lore_B, float* y_slots, float* y_shared, void* ws,
+                                         size_t ws_bytes, spice_stream_t stream);
 
 /*
  * Step 4: LoRE correction delta = B_e (A_e x) (Eq. 9) for every LORE slot, grouped by

@@ -1,5 +1,5 @@
 // Exact CPU residual for exact-miss slots (Sec. 4.3: the M_cpu part of Eq. 12).
-// Expert weights are in the cfg dtype, or MXFP4 blobs (cfg.wfmt), decoded on the fly.
+// Expert weights are in the cfg dtype, MXFP4 blobs or 8-bit blobs (cfg.wfmt), decoded on the fly.
 //
 // resid[t] = sum_{k in EXACT(t)} g[t][k] * W2_e (silu(W1_e x_t) * (W3_e x_t)),
 // computed from host-resident expert weights.  Work is grouped by expert so each
@@ -136,8 +136,11 @@ class Pool {
 };
 
 // ------------------------------------------------------------ dot products
-// out[j] = sum_i w[i] * xs[j*ld + i] for j < n; w has `len` elements (dtype).
+// out[j] = sum_i w[i] * xs[j*ld + i] for j < n; w has `len` elements (dtype, or kInt8: 8-bit codes).
+constexpr int kInt8 = 1000;
+
 inline float load_w(const void* w, int dtype, size_t i) {
+    if (dtype == kInt8) return (float)static_cast<const int8_t*>(w)[i];
     if (dtype == SPICE_BF16) {
         uint32_t b = (uint32_t)static_cast<const uint16_t*>(w)[i] << 16;
         float f;
@@ -160,6 +163,10 @@ void dots_generic(const void* w, int dtype, size_t len, const float* xs, size_t 
 
 __attribute__((target("avx512f,avx512bw,avx512vl,fma"))) inline __m512 load16_avx512(const void* w, int dtype,
                                                                                        size_t i) {
+    if (dtype == kInt8) {
+        const __m128i b = _mm_loadu_si128(reinterpret_cast<const __m128i*>(static_cast<const int8_t*>(w) + i));
+        return _mm512_cvtepi32_ps(_mm512_cvtepi8_epi32(b));
+    }
     if (dtype == SPICE_BF16) {
         const __m256i b = _mm256_loadu_si256(reinterpret_cast<const __m256i*>(static_cast<const uint16_t*>(w) + i));
         return _mm512_castsi512_ps(_mm512_slli_epi32(_mm512_cvtepu16_epi32(b), 16));
@@ -377,7 +384,8 @@ extern "C" spice_status_t moe_exact_residual_host(const spice_moe_cfg_t* cfg, in
         int threads = n_threads > 0 ? n_threads : (int)std::max(1u, std::thread::hardware_concurrency());
         static const DotsFn dots = pick_dots();
         static const DotsMxFn dots_mx = pick_dots_mx();
-        const bool mx = c.wfmt == SPICE_WFMT_MXFP4;
+        const bool mx = c.wfmt == SPICE_WFMT_MXFP4, i8 = c.wfmt == SPICE_WFMT_INT8;
+        const int wdt = i8 ? kInt8 : dt;  // what the weight rows hold
         Pool& pool = Pool::get();
 
         // x rows of the exact slots, widened to fp32 (one row per slot)
@@ -389,7 +397,7 @@ extern "C" spice_status_t moe_exact_residual_host(const spice_moe_cfg_t* cfg, in
 
         constexpr int kRows1 = 32, kRows2 = 64;
         const int nb1 = (I + kRows1 - 1) / kRows1, nb2 = (d + kRows2 - 1) / kRows2;
-        const size_t es = dt == SPICE_BF16 ? 2 : 4;
+        const size_t es = i8 ? 1 : dt == SPICE_BF16 ? 2 : 4;
         const int ne = (int)experts.size();
 
         pool.run(ne * nb1, threads, [&](int task) {
@@ -407,8 +415,16 @@ extern "C" spice_status_t moe_exact_residual_host(const spice_moe_cfg_t* cfg, in
                     dots_mx(el + (size_t)(I + i) * (d / 2), sc + (size_t)(I + i) * (d / 32), d,
                             &xs[(size_t)base * d], d, n, uv.data());
                 } else {
-                    dots(w13 + (size_t)i * d * es, dt, d, &xs[(size_t)base * d], d, n, gv.data());
-                    dots(w13 + (size_t)(I + i) * d * es, dt, d, &xs[(size_t)base * d], d, n, uv.data());
+                    dots(w13 + (size_t)i * d * es, wdt, d, &xs[(size_t)base * d], d, n, gv.data());
+                    dots(w13 + (size_t)(I + i) * d * es, wdt, d, &xs[(size_t)base * d], d, n, uv.data());
+                }
+                if (i8) {  // the rows' scales, behind the codes
+                    const char* sc8 = w13 + (size_t)2 * I * d;
+                    const float s1 = load_w(sc8, SPICE_F32, i), s3 = load_w(sc8, SPICE_F32, I + i);
+                    for (int j = 0; j < n; ++j) {
+                        gv[j] *= s1;
+                        uv[j] *= s3;
+                    }
                 }
                 for (int j = 0; j < n; ++j) h[(size_t)(base + j) * I + i] = silu(gv[j]) * uv[j];
             }
@@ -425,7 +441,11 @@ extern "C" spice_status_t moe_exact_residual_host(const spice_moe_cfg_t* cfg, in
                     dots_mx(el + (size_t)j * (I / 2), sc + (size_t)j * (I / 32), I, &h[(size_t)base * I], I, n,
                             ov.data());
                 else
-                    dots(w2 + (size_t)j * I * es, dt, I, &h[(size_t)base * I], I, n, ov.data());
+                    dots(w2 + (size_t)j * I * es, wdt, I, &h[(size_t)base * I], I, n, ov.data());
+                if (i8) {
+                    const float s2 = load_w(w2 + (size_t)d * I, SPICE_F32, j);
+                    for (int q = 0; q < n; ++q) ov[q] *= s2;
+                }
                 for (int q = 0; q < n; ++q) y[(size_t)(base + q) * d + j] = ov[q];
             }
         });

@@ -44,7 +44,7 @@ constexpr size_t kLogitLdsBytes = sizeof(TopkLds) > bucket_lds_bytes(kLogitThrea
 
 typedef double f64x4_t __attribute__((ext_vector_type(4)));
 
-template <int DT>
+template <int DT, bool kScored>
 __global__ __launch_bounds__(kLogitThreads) void route_logits_kernel(RouteArgs a, int g_per_tok) {
     __shared__ __align__(16) int s_lds[kLogitLdsBytes / sizeof(int)];
     __shared__ int s_flag;
@@ -53,7 +53,7 @@ __global__ __launch_bounds__(kLogitThreads) void route_logits_kernel(RouteArgs a
     const int n_rows = a.N + (a.w_sg ? 1 : 0);
     route_logits_rows<DT>(a, t, g * rows, min(n_rows, (g + 1) * rows));
     if (!route_last_block(&a.ctrl[kWordTokCount + t * kTokCountStride], g_per_tok, &s_flag)) return;
-    block_topk<kLogitThreads, true, true>(a, t, a.logits_ws + (size_t)t * a.N, *reinterpret_cast<TopkLds*>(s_lds));
+    block_topk<kLogitThreads, true, true, kScored>(a, t, a.logits_ws + (size_t)t * a.N, *reinterpret_cast<TopkLds*>(s_lds));
     // the published top-K outputs and keys of every token are at the device-coherent level
     // once every token's last block has counted itself here
     if (!route_last_block(&a.ctrl[kWordRouteDone], a.T, &s_flag)) return;
@@ -163,7 +163,7 @@ constexpr size_t kTiledBucketLds = bucket_lds_bytes(kPrefillThreads, SPICE_MAX_E
 // contraction; the last of the group's blocks adds the parts in order), top-K, gates, classes.
 // kOne: the last block over all groups then buckets the slots (few tokens); otherwise the
 // group's histogram of bucket keys goes to column b / parts of the table.
-template <int DT, bool kOne>
+template <int DT, bool kOne, bool kScored>
 __global__ __launch_bounds__(kPrefillThreads) void route_tiled_kernel(RouteArgs a, int parts_k) {
     __shared__ __align__(16) unsigned char s_raw[sizeof(PrefillLds) > kTiledBucketLds ? sizeof(PrefillLds) : kTiledBucketLds];
     __shared__ int s_flag;
@@ -248,6 +248,12 @@ __global__ __launch_bounds__(kPrefillThreads) void route_tiled_kernel(RouteArgs 
     for (int h = 0; h < kPrefillTok / kNW; ++h) {
         const int tt = w + h * kNW;
         const unsigned long long* kr = L.key[tt];
+        if constexpr (kScored) {
+            // the partial logits are summed: their region holds the waves' group values
+            static_assert(sizeof(GroupLds) * kNW <= sizeof(L.zp), "group values fit the partial logits' region");
+            score_experts<WaveTeam>(a, L.z[tt], L.key[tt], reinterpret_cast<GroupLds*>(L.zp)[w]);
+            WaveTeam::sync();
+        }
 #pragma unroll
         for (int j = 0; j < kJ; ++j) {
             const int e = lane + 64 * j;
@@ -270,7 +276,7 @@ __global__ __launch_bounds__(kPrefillThreads) void route_tiled_kernel(RouteArgs 
         const int tt = w + h * kNW, t = t0 + tt;
         if (t < a.T) {
             const float conf_in = (a.conf_mode == SPICE_CONF_INPUT && lane < K) ? a.conf[(size_t)t * K + lane] : 0.f;
-            const int key = wave_topk_gates<kOne>(a, t, L.z[tt], L.res, L.pick[tt], lane, conf_in);
+            const int key = wave_topk_gates<kOne, kScored>(a, t, L.z[tt], L.res, L.pick[tt], lane, conf_in);
             if (!kOne && key >= 0) atomicAdd(&L.hist[key], 1);
         }
     }
@@ -437,34 +443,34 @@ __global__ __launch_bounds__(64) void bucket_scatter_kernel(RouteArgs a) {
 
 }  // namespace
 
-hipError_t launch_route_bucket(const RouteArgs& a, hipStream_t s) {
+namespace {
+
+template <int DT, bool kScored>
+hipError_t launch_route(const RouteArgs& a, hipStream_t s) {
     const unsigned groups = (unsigned)((a.T + kPrefillTok - 1) / kPrefillTok);
     const int parts = route_parts(a.T, a.N, a.d, a.dtype, a.part_bytes);
     if (route_keeps_rows(a.T, a.N, a.d, parts, a.hx != nullptr)) {
         const int g = route_blocks_per_token(a.N + (a.w_sg ? 1 : 0), kLogitThreads);
-        const dim3 grid((unsigned)(a.T * g));
-        if (a.dtype == SPICE_BF16)
-            hipLaunchKernelGGL(route_logits_kernel<SPICE_BF16>, grid, dim3(kLogitThreads), 0, s, a, g);
-        else
-            hipLaunchKernelGGL(route_logits_kernel<SPICE_F32>, grid, dim3(kLogitThreads), 0, s, a, g);
+        hipLaunchKernelGGL((route_logits_kernel<DT, kScored>), dim3((unsigned)(a.T * g)), dim3(kLogitThreads), 0, s, a, g);
         return hipGetLastError();
     }
     const dim3 grid(groups * (unsigned)parts);
     if (a.T <= kRouteTokenMaxT) {
-        if (a.dtype == SPICE_BF16)
-            hipLaunchKernelGGL((route_tiled_kernel<SPICE_BF16, true>), grid, dim3(kPrefillThreads), 0, s, a, parts);
-        else
-            hipLaunchKernelGGL((route_tiled_kernel<SPICE_F32, true>), grid, dim3(kPrefillThreads), 0, s, a, parts);
+        hipLaunchKernelGGL((route_tiled_kernel<DT, true, kScored>), grid, dim3(kPrefillThreads), 0, s, a, parts);
         return hipGetLastError();
     }
-    if (a.dtype == SPICE_BF16)
-        hipLaunchKernelGGL((route_tiled_kernel<SPICE_BF16, false>), grid, dim3(kPrefillThreads), 0, s, a, parts);
-    else
-        hipLaunchKernelGGL((route_tiled_kernel<SPICE_F32, false>), grid, dim3(kPrefillThreads), 0, s, a, parts);
+    hipLaunchKernelGGL((route_tiled_kernel<DT, false, kScored>), grid, dim3(kPrefillThreads), 0, s, a, parts);
     hipLaunchKernelGGL(bucket_scan_kernel, dim3((unsigned)((3 * a.N + kScanKeys - 1) / kScanKeys)), dim3(kScanThreads), 0, s,
                        a);
     hipLaunchKernelGGL(bucket_scatter_kernel, dim3(groups), dim3(64), 0, s, a);
     return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_route_bucket(const RouteArgs& a, hipStream_t s) {
+    if (a.dtype == SPICE_BF16) return a.scored ? launch_route<SPICE_BF16, true>(a, s) : launch_route<SPICE_BF16, false>(a, s);
+    return a.scored ? launch_route<SPICE_F32, true>(a, s) : launch_route<SPICE_F32, false>(a, s);
 }
 
 }  // namespace spice

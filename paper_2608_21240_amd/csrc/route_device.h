@@ -4,6 +4,8 @@
 //
 //   route_logits_rows : fp64 logits of one token against a range of router rows, by one
 //                       block (a token's rows are spread over route_blocks_per_token blocks);
+//   score_experts : another scoring rule (moe_route_bucket_scored): scores, groups and the
+//                  choice keys of one token, by a block or a wave;
 //   block_topk   : softmax over the N logits, the K largest (descending, the lower id wins
 //                  ties), gate, confidence and class of each of the K slots, by one block;
 //   bucket_slots : stable counting sort of the T*K slots by key (class, expert), the
@@ -169,6 +171,96 @@ __device__ __forceinline__ unsigned long long logit_key(double z) {
     return (u >> 63) ? ~u : (u | 0x8000000000000000ull);
 }
 
+// Confidence and class of a slot and its outputs, by lane k < K of a wave: expert my_e, gate g, weight
+// w_out; gsum: the K gates' sum (conf_mode GATE_RENORM).  Returns the slot's bucket key (class * N +
+// expert).  kPublish: the outputs and the key (control word kWordSlotKeys + slot) are written through
+// to the device-coherent level, for a block of the same launch on another XCD.
+template <bool kPublish>
+__device__ __forceinline__ int slot_outputs(const RouteArgs& a, int t, const int* res, int lane, int my_e, double g,
+                                            double gsum, float w_out, float conf_in) {
+    const int N = a.N;
+    const size_t s = (size_t)t * a.K + lane;
+    float conf;
+    if (a.conf_mode == SPICE_CONF_INPUT) conf = conf_in;
+    else if (a.conf_mode == SPICE_CONF_GATE) conf = (float)g;
+    else conf = (float)(g / gsum);
+    int32_t slot = res[my_e];
+    if (slot < -1 || slot >= a.C) {
+        atomicOr(&a.ctrl[kWordFlags], (uint32_t)SPICE_FLAG_BAD_SLOT);
+        slot = -1;
+    }
+    uint8_t cls;
+    if (slot >= 0) cls = SPICE_CLASS_HIT;
+    else if (conf < a.tau) cls = SPICE_CLASS_LORE;
+    else cls = SPICE_CLASS_EXACT;
+    if (kPublish) {
+        __hip_atomic_store(a.topk_idx + s, my_e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(a.topk_w + s, w_out, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(a.slot_class + s, cls, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(a.ctrl + kWordSlotKeys + s, (uint32_t)(cls * N + my_e), __ATOMIC_RELAXED,
+                           __HIP_MEMORY_SCOPE_AGENT);
+    } else {
+        a.topk_idx[s] = my_e;
+        a.topk_w[s] = w_out;
+        a.slot_class[s] = cls;
+    }
+    return cls * N + my_e;
+}
+
+// The gates, confidence and classes of token t's K picks, by one wave: z = its N logits (kScored: its
+// N scores), res = resident_slot, pick = its experts in rank order (all in LDS).  Lane k < K returns
+// its slot's bucket key, the other lanes -1.
+template <bool kPublish = false, bool kScored = false>
+__device__ int wave_topk_gates(const RouteArgs& a, int t, const double* z, const int* res, const int* pick,
+                               int lane, float conf_in) {
+    constexpr int kJ = SPICE_MAX_EXPERTS / 64;
+    const int N = a.N, K = a.K;
+    const int my_e = lane < K ? pick[lane] : 0;
+    if constexpr (kScored) {
+        double g = lane < K ? z[my_e] : 0.0;
+        const double sum = (a.norm_topk || a.conf_mode == SPICE_CONF_GATE_RENORM) ? route_wave_sum(g) : 1.0;
+        if (a.norm_topk) g = sum > 0.0 ? g / sum : 0.0;
+        const double gsum = a.norm_topk || !(sum > 0.0) ? 1.0 : sum;
+        if (lane >= K) return -1;
+        return slot_outputs<kPublish>(a, t, res, lane, my_e, g, gsum, (float)(g * (double)a.scale), conf_in);
+    }
+    const double m = z[pick[0]];  // the largest logit
+    double part = 0.0;
+#pragma unroll
+    for (int j = 0; j < kJ; ++j)
+        if (lane + 64 * j < N) part += exp(z[lane + 64 * j] - m);
+    const double my_ex = lane < K ? exp(z[my_e] - m) : 0.0;
+    const double denom = route_wave_sum(part);
+    double g = my_ex / denom;
+    if (a.norm_topk) g = g / route_wave_sum(lane < K ? g : 0.0);
+    const double gsum = (a.conf_mode == SPICE_CONF_GATE_RENORM) ? route_wave_sum(lane < K ? g : 0.0) : 1.0;
+    if (lane >= K) return -1;
+    return slot_outputs<kPublish>(a, t, res, lane, my_e, g, gsum, (float)g, conf_in);
+}
+
+// The threads that score one token together: a block of NT, or one wave.
+template <int NT>
+struct BlockTeam {
+    static constexpr int n = NT;
+    __device__ static int id() { return threadIdx.x; }
+    __device__ static void sync() { __syncthreads(); }
+};
+struct WaveTeam {
+    static constexpr int n = 64;
+    __device__ static int id() { return threadIdx.x & 63; }
+    // a wave's LDS accesses complete in order; only the compiler has to keep theirs
+    __device__ static void sync() {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+};
+
+// LDS of score_experts for one token.
+struct GroupLds {
+    double best[kMaxGroups], second[kMaxGroups];  // a group's two largest choice values
+    int keep[kMaxGroups];
+};
+
 // LDS of block_topk.
 struct TopkLds {
     double z[SPICE_MAX_EXPERTS];
@@ -176,58 +268,83 @@ struct TopkLds {
     int res[SPICE_MAX_EXPERTS];
     int rank[SPICE_MAX_EXPERTS];
     int pick[64];
+    GroupLds group;  // scored calls
 };
 
-// The gates, confidence and classes of token t's K picks, by one wave: z = its N logits,
-// res = resident_slot, pick = its experts in rank order (all in LDS).  Lane k < K returns
-// its slot's bucket key (class * N + expert), the other lanes -1.  kPublish: the outputs
-// and the key (control word kWordSlotKeys + slot) are written through to the
-// device-coherent level, for a block of the same launch on another XCD.
-template <bool kPublish = false>
-__device__ int wave_topk_gates(const RouteArgs& a, int t, const double* z, const int* res, const int* pick,
-                               int lane, float conf_in) {
+// Scores and choice keys of one token by a team (moe_route_bucket_scored): z = its N logits in, its
+// scores out; key = the order-preserving keys of the choice values, 0 for experts of groups that are
+// not kept (every other key is larger).  Every wave sums the softmax for itself, so no team
+// reduction is needed; a group's two largest values are found by each member's rank in its group.
+// The caller syncs before (z is there) and after (keys and scores are).
+template <class Team>
+__device__ void score_experts(const RouteArgs& a, double* z, unsigned long long* key, GroupLds& G) {
     constexpr int kJ = SPICE_MAX_EXPERTS / 64;
-    const int N = a.N, K = a.K;
-    const double m = z[pick[0]];  // the largest logit
-    double part = 0.0;
+    const int N = a.N, id = Team::id(), lane = threadIdx.x & 63;
+    const double ninf = -INFINITY;
+    double m = ninf, inv = 1.0;
+    if (!a.sigmoid) {
+        double v[kJ];
 #pragma unroll
-    for (int j = 0; j < kJ; ++j)
-        if (lane + 64 * j < N) part += exp(z[lane + 64 * j] - m);
-    const int my_e = lane < K ? pick[lane] : 0;
-    const double my_ex = lane < K ? exp(z[my_e] - m) : 0.0;
-    const double denom = route_wave_sum(part);
-    double g = my_ex / denom;
-    if (a.norm_topk) g = g / route_wave_sum(lane < K ? g : 0.0);
-    const double gsum = (a.conf_mode == SPICE_CONF_GATE_RENORM) ? route_wave_sum(lane < K ? g : 0.0) : 1.0;
-    if (lane < K) {
-        const size_t s = (size_t)t * K + lane;
-        float conf;
-        if (a.conf_mode == SPICE_CONF_INPUT) conf = conf_in;
-        else if (a.conf_mode == SPICE_CONF_GATE) conf = (float)g;
-        else conf = (float)(g / gsum);
-        int32_t slot = res[my_e];
-        if (slot < -1 || slot >= a.C) {
-            atomicOr(&a.ctrl[kWordFlags], (uint32_t)SPICE_FLAG_BAD_SLOT);
-            slot = -1;
+        for (int j = 0; j < kJ; ++j) {
+            v[j] = lane + 64 * j < N ? z[lane + 64 * j] : ninf;
+            m = fmax(m, v[j]);
         }
-        uint8_t cls;
-        if (slot >= 0) cls = SPICE_CLASS_HIT;
-        else if (conf < a.tau) cls = SPICE_CLASS_LORE;
-        else cls = SPICE_CLASS_EXACT;
-        if (kPublish) {
-            __hip_atomic_store(a.topk_idx + s, my_e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            __hip_atomic_store(a.topk_w + s, (float)g, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            __hip_atomic_store(a.slot_class + s, cls, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            __hip_atomic_store(a.ctrl + kWordSlotKeys + s, (uint32_t)(cls * N + my_e), __ATOMIC_RELAXED,
-                               __HIP_MEMORY_SCOPE_AGENT);
-        } else {
-            a.topk_idx[s] = my_e;
-            a.topk_w[s] = (float)g;
-            a.slot_class[s] = cls;
-        }
-        return cls * N + my_e;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) m = fmax(m, __shfl_xor(m, o));
+        double part = 0.0;
+#pragma unroll
+        for (int j = 0; j < kJ; ++j)
+            if (64 * j < N && v[j] != ninf) part += exp(v[j] - m);
+        inv = 1.0 / route_wave_sum(part);  // a token whose logits are all -inf: no expert reads it
+        Team::sync();  // every wave has read the logits
     }
-    return -1;
+    const int per = N / a.n_group;
+    for (int e = id; e < N; e += Team::n) {
+        const double ze = z[e];
+        const bool masked = ze == ninf;
+        const double s = masked ? 0.0 : a.sigmoid ? 1.0 / (1.0 + exp(-ze)) : exp(ze - m) * inv;
+        const double c = masked ? ninf : a.balance ? s + (double)a.balance[e] : s;
+        z[e] = s;
+        const unsigned long long k = logit_key(c);
+        key[e] = k ? k : 1ull;
+    }
+    if (a.n_group == 1) return;
+    Team::sync();
+    const unsigned long long kmask = logit_key(ninf);
+    for (int e = id; e < N; e += Team::n) {
+        const int g = e / per, e0 = g * per;
+        const unsigned long long k = key[e];
+        int r = 0;
+#pragma unroll 8
+        for (int i = 0; i < per; ++i) {
+            const unsigned long long k2 = key[e0 + i];
+            r += (int)((k2 > k) | ((k2 == k) & (e0 + i < e)));
+        }
+        if (r < 2) {
+            const double c = k == kmask ? ninf : a.balance ? z[e] + (double)a.balance[e] : z[e];
+            if (r == 0) G.best[g] = c;
+            else G.second[g] = c;
+        }
+    }
+    Team::sync();
+    auto value = [&](int g) {
+        double v = G.best[g];
+        if (a.group_top == 2 && per > 1 && G.second[g] != ninf) v += G.second[g];
+        const unsigned long long k = logit_key(v);
+        return k;
+    };
+    for (int g = id; g < a.n_group; g += Team::n) {
+        const unsigned long long k = value(g);
+        int r = 0;
+        for (int i = 0; i < a.n_group; ++i) {
+            const unsigned long long k2 = value(i);
+            r += (int)((k2 > k) | ((k2 == k) & (i < g)));
+        }
+        G.keep[g] = r < a.topk_group;
+    }
+    Team::sync();
+    for (int e = id; e < N; e += Team::n)
+        if (!G.keep[e / per]) key[e] = 0ull;
 }
 
 // Top-K of token t from its N logits zg (fp64, bias included; global memory) by one block
@@ -236,8 +353,8 @@ __device__ int wave_topk_gates(const RouteArgs& a, int t, const double* z, const
 // experts ee against every e, and rank k < K makes e the k-th pick (descending, the lower id
 // wins ties).  Then the softmax over all N, the gate of each pick (its probability,
 // optionally renormalised over the K), its confidence and its class (kPublish: see
-// wave_topk_gates).
-template <int NT, bool kCoherent, bool kPublish = false>
+// slot_outputs).  kScored: the scores and choice keys of score_experts take the logits' place.
+template <int NT, bool kCoherent, bool kPublish = false, bool kScored = false>
 __device__ void block_topk(const RouteArgs& a, int t, const double* zg, TopkLds& L) {
     constexpr int NW = NT / 64;
     constexpr int kJ = SPICE_MAX_EXPERTS / 64;
@@ -252,12 +369,16 @@ __device__ void block_topk(const RouteArgs& a, int t, const double* zg, TopkLds&
                             reinterpret_cast<const unsigned long long*>(zg) + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT))
                       : zg[e];
         L.z[e] = z;
-        L.key[e] = logit_key(z);
+        if (!kScored) L.key[e] = logit_key(z);
         L.res[e] = a.resident_slot[e];
         L.rank[e] = 0;
     }
     const float conf_in = (a.conf_mode == SPICE_CONF_INPUT && tid < K) ? a.conf[(size_t)t * K + tid] : 0.f;
     __syncthreads();
+    if constexpr (kScored) {
+        score_experts<BlockTeam<NT>>(a, L.z, L.key, L.group);
+        __syncthreads();
+    }
     const int e_lo = w * N / NW, e_hi = (w + 1) * N / NW;  // this wave's share of the experts ee
 #pragma unroll
     for (int j = 0; j < kJ; ++j) {
@@ -277,7 +398,7 @@ __device__ void block_topk(const RouteArgs& a, int t, const double* zg, TopkLds&
     for (int e = tid; e < N; e += NT)
         if (L.rank[e] < K) L.pick[L.rank[e]] = e;
     __syncthreads();
-    if (w == 0) wave_topk_gates<kPublish>(a, t, L.z, L.res, L.pick, lane, conf_in);
+    if (w == 0) wave_topk_gates<kPublish, kScored>(a, t, L.z, L.res, L.pick, lane, conf_in);
 }
 
 // The last of a token's routing blocks to finish, found with an arrival counter.  A block's

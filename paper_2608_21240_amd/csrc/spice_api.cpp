@@ -45,8 +45,14 @@ spice_status_t check_cfg(const spice_moe_cfg_t* c) {
     if (c->norm_topk != 0 && c->norm_topk != 1) return fail(SPICE_ERR_INVALID, "norm_topk must be 0 or 1");
     if (c->conf_mode < SPICE_CONF_INPUT || c->conf_mode > SPICE_CONF_GATE_RENORM)
         return fail(SPICE_ERR_INVALID, "conf_mode must be a SPICE_CONF_* value");
-    if (c->wfmt != SPICE_WFMT_DTYPE && c->wfmt != SPICE_WFMT_MXFP4)
-        return fail(SPICE_ERR_INVALID, "wfmt must be SPICE_WFMT_DTYPE or SPICE_WFMT_MXFP4");
+    if (c->wfmt != SPICE_WFMT_DTYPE && c->wfmt != SPICE_WFMT_MXFP4 && c->wfmt != SPICE_WFMT_INT8)
+        return fail(SPICE_ERR_INVALID, "wfmt must be a SPICE_WFMT_* value");
+    if (c->wfmt == SPICE_WFMT_INT8 && c->dtype != SPICE_BF16)
+        return fail(SPICE_ERR_UNSUPPORTED, "8-bit expert weights need dtype SPICE_BF16");
+    if (c->wfmt == SPICE_WFMT_INT8 && (c->d % 16 || c->inter % 16 || c->shared_inter % 16))
+        return fail(SPICE_ERR_UNSUPPORTED, "8-bit expert weights need d, inter and shared_inter multiples of 16");
+    if (c->wfmt == SPICE_WFMT_INT8 && (c->inter > SPICE_INT8_MAX_K || c->shared_inter > SPICE_INT8_MAX_K))
+        return fail(SPICE_ERR_UNSUPPORTED, "8-bit expert weights need inter and shared_inter at most SPICE_INT8_MAX_K");
     if (c->wfmt == SPICE_WFMT_MXFP4 && c->dtype != SPICE_BF16)
         return fail(SPICE_ERR_UNSUPPORTED, "MXFP4 expert weights need dtype SPICE_BF16");
     if (c->wfmt == SPICE_WFMT_MXFP4 && (c->d % 32 || c->inter % 32))
@@ -164,10 +170,15 @@ WsLayout ws_layout(const spice_moe_cfg_t& c, int32_t T) {
     const size_t t = (size_t)std::max(T, 0), slots = t * (size_t)c.top_k, es = elem_size(c);
     size_t off = SPICE_WS_CONTROL_BYTES;
     L.logits = off; off += align256(t * (size_t)c.n_experts * sizeof(double));
-    L.h = off;      off += align256(slots * ((size_t)c.inter + kHPad) * es);
-    L.hs = off;     off += align256(t * ((size_t)c.shared_inter + kHPad) * es);
+    const bool i8 = c.wfmt == SPICE_WFMT_INT8;
+    L.h = off;      off += align256(i8 ? slots * (size_t)c.inter * 4 : slots * ((size_t)c.inter + kHPad) * es);
+    L.hs = off;     off += align256(i8 ? t * (size_t)c.shared_inter * 4 : t * ((size_t)c.shared_inter + kHPad) * es);
     L.u = off;      off += align256(slots * (size_t)c.lore_rank * sizeof(float));
     L.sgate = off;  off += align256(t * sizeof(float));
+    L.hq = off;     off += i8 ? align256(slots * i8_row(c.inter)) : 0;
+    L.hqs = off;    off += i8 ? align256(t * i8_row(c.shared_inter)) : 0;
+    L.hscale = off;   off += i8 ? align256(slots * sizeof(float)) : 0;
+    L.hscale_s = off; off += i8 ? align256(t * sizeof(float)) : 0;
     L.base = off;
     L.zpart = off;
     if (T >= kRouteTiledMinT) {
@@ -279,6 +290,42 @@ spice_status_t moe_route_bucket(const spice_moe_cfg_t* cfg, int32_t T, const voi
     SPICE_TRY_END
 }
 
+spice_status_t moe_route_bucket_scored(const spice_moe_cfg_t* cfg, const spice_route_score_t* score, int32_t T,
+                                       const void* x, const void* w_gate, const float* logit_bias,
+                                       const int32_t* resident_slot, const float* conf, double* logits,
+                                       int32_t* topk_idx, float* topk_w, uint8_t* slot_class, int32_t* offsets,
+                                       int32_t* perm, int32_t* inv_perm, const spice_host_out_t* host_out, void* ws,
+                                       size_t ws_bytes, spice_stream_t stream) {
+    SPICE_TRY_BEGIN
+    SPICE_REQUIRE(score, "score");
+    spice::RouteArgs a{};
+    spice_status_t st = prep_route(cfg, T, x, w_gate, logit_bias, resident_slot, conf, logits, topk_idx, topk_w,
+                                   slot_class, offsets, perm, inv_perm, host_out, ws, ws_bytes, a);
+    if (st != SPICE_OK) return st;
+    const int N = cfg->n_experts, G = score->n_group;
+    if (score->score != SPICE_SCORE_SOFTMAX && score->score != SPICE_SCORE_SIGMOID)
+        return fail(SPICE_ERR_INVALID, "moe_route_bucket_scored: score must be a SPICE_SCORE_* value");
+    if (G < 1 || N % G)
+        return fail(SPICE_ERR_INVALID, "moe_route_bucket_scored: n_group must be positive and divide n_experts");
+    if (G > spice::kMaxGroups) return fail(SPICE_ERR_UNSUPPORTED, "moe_route_bucket_scored: n_group above 64");
+    if (score->topk_group < 1 || score->topk_group > G)
+        return fail(SPICE_ERR_INVALID, "moe_route_bucket_scored: topk_group must be in [1, n_group]");
+    if (score->group_top != 1 && score->group_top != 2)
+        return fail(SPICE_ERR_INVALID, "moe_route_bucket_scored: group_top must be 1 or 2");
+    if (score->topk_group * (N / G) < cfg->top_k)
+        return fail(SPICE_ERR_INVALID, "moe_route_bucket_scored: the kept groups hold fewer than top_k experts");
+    if (!std::isfinite(score->scale)) return fail(SPICE_ERR_INVALID, "moe_route_bucket_scored: scale must be finite");
+    if (T == 0) return SPICE_OK;
+    a.scored = 1;
+    a.sigmoid = score->score == SPICE_SCORE_SIGMOID;
+    a.n_group = G; a.topk_group = score->topk_group; a.group_top = score->group_top;
+    a.scale = score->scale; a.balance = score->balance_bias;
+    hipError_t e = spice::launch_route_bucket(a, stream);
+    if (e != hipSuccess) return hip_fail(e, "moe_route_bucket_scored");
+    return SPICE_OK;
+    SPICE_TRY_END
+}
+
 }  // extern "C"
 
 namespace {
@@ -293,6 +340,8 @@ spice_status_t prep_ffn(const spice_moe_cfg_t* cfg, int32_t T, const void* x, co
     if (st != SPICE_OK) return st;
     const spice_moe_cfg_t& c = *cfg;
     if ((st = check_tokens(c, T)) != SPICE_OK) return st;
+    if (c.wfmt == SPICE_WFMT_INT8 && (groups & (spice::kDoHit | spice::kDoShared)))
+        return fail(SPICE_ERR_UNSUPPORTED, std::string(name) + ": 8-bit experts take moe_expert_ffn_grouped_i8");
     if (T == 0) return SPICE_OK;
     SPICE_REQUIRE(x, "x");
     SPICE_REQUIRE(perm, "perm");

@@ -21,6 +21,8 @@ constexpr int kWordTokCount = 4096;
 constexpr int kTokCountStride = 32;  // words between two tokens' counters
 static_assert(kWordWorkList + 3 * SPICE_MAX_EXPERTS * 4 <= kWordTokCount, "work lists overlap the counters");
 
+// Most expert groups of a scored routing call.
+constexpr int kMaxGroups = 64;
 // Largest T whose routing call is one launch.
 constexpr int kRouteTokenMaxT = 256;
 // Fewest tokens whose logits may be computed as fp64 MFMA tiles of 16 tokens (route_bucket.hip).
@@ -75,6 +77,9 @@ struct WsLayout {
     size_t hs;      // shared-block intermediate [T][I_s + kHPad] (dtype)
     size_t u;       // LoRE A x, fp32 [T*K][r]
     size_t sgate;   // output gate of the shared block, fp32 [T]
+    // 8-bit experts (SPICE_WFMT_INT8; h and hs are fp32 there): the requantised intermediates, int8
+    // [T*K][i8_row(I)] and [T][i8_row(I_s)], and their scales, fp32 [T*K] and [T]
+    size_t hq, hqs, hscale, hscale_s;
     size_t base;    // bytes every call needs; the rest is used when the workspace has it
     size_t zpart;   // partial logits of the tiled routing, fp64 (its own: no FFN buffer is touched by a routing call)
     size_t part;    // the shared block's partial results, fp32 [parts][T][d]
@@ -84,6 +89,10 @@ WsLayout ws_layout(const spice_moe_cfg_t& c, int32_t T);
 
 // Which expert groups a grouped-FFN launch covers.
 enum : int { kDoHit = 1, kDoShared = 2, kDoLore = 4 };
+
+// Row stride (bytes) of the 8-bit intermediates: rows start on a 128-byte line, an odd number of
+// lines apart, so that the rows of a tile spread over the channels.
+inline __host__ __device__ size_t i8_row(int32_t K) { return (((size_t)K + 127) / 128 | 1) * 128; }
 
 struct RouteArgs {
     int32_t T, d, N, K, C, dtype, norm_topk, conf_mode;
@@ -106,6 +115,10 @@ struct RouteArgs {
     uint32_t* ctrl;       // workspace control words
     int32_t* worklist;    // [3][N][4] work records (control region)
     int32_t* wl_count;    // [3] their lengths (control region)
+    // scoring rule of moe_route_bucket_scored; the plain call's (softmax, no groups) when !scored
+    int32_t scored, sigmoid, n_group, topk_group, group_top;
+    float scale;
+    const float* balance;  // [N], nullable
     const void* w_sg;     // nullable: the shared block's gate row [d]; sgate[t] = sigmoid(w_sg . x[t])
     float* sgate;         // [T], written when w_sg is set
     // device-visible addresses of the caller's pinned host copies (each nullable)
@@ -121,10 +134,12 @@ struct RouteArgs {
 // Bytes of one routed expert's W13 [2I][d] and W2 [d][I] in the cfg's weight format.
 inline size_t expert_w13_bytes(const spice_moe_cfg_t& c) {
     const size_t n = (size_t)2 * c.inter * c.d;
+    if (c.wfmt == SPICE_WFMT_INT8) return n + (size_t)8 * c.inter;
     return c.wfmt == SPICE_WFMT_MXFP4 ? n / 2 + n / 32 : n * (c.dtype == SPICE_BF16 ? 2 : 4);
 }
 inline size_t expert_w2_bytes(const spice_moe_cfg_t& c) {
     const size_t n = (size_t)c.inter * c.d;
+    if (c.wfmt == SPICE_WFMT_INT8) return n + (size_t)4 * c.d;
     return c.wfmt == SPICE_WFMT_MXFP4 ? n / 2 + n / 32 : n * (c.dtype == SPICE_BF16 ? 2 : 4);
 }
 
@@ -181,6 +196,43 @@ struct SpecArgs {
     int32_t* h_pred_idx;
     float* h_pred_prob;
     float* h_conf;
+};
+
+// The 8-bit expert FFN (expert_ffn_i8.hip).
+struct FfnI8Args {
+    int32_t T, d, N, K, C, I, Is;
+    const int8_t* xq;
+    const float* xs;
+    const int32_t* perm;
+    const int32_t* offsets;
+    const int32_t* resident_slot;
+    const char* w13_pool;
+    const char* w2_pool;
+    const char* w13s;
+    const char* w2s;
+    const float* sgate;     // nullable, as in FfnArgs
+    float* y_slots;
+    float* y_shared;
+    float* h;               // workspace [T*K][I]
+    float* hs;              // workspace [T][I_s]
+    int8_t* hq;             // workspace [T*K][i8_row(I)]
+    int8_t* hqs;            // workspace [T][i8_row(I_s)]
+    float* hscale;          // workspace [T*K]
+    float* hscale_s;        // workspace [T]
+    uint32_t* ctrl;
+};
+
+// RMS norm with the residual's addition and 8-bit output (rmsnorm_quant.hip).
+struct NormArgs {
+    int32_t T, d, dtype;
+    double eps;
+    const void* x;
+    const void* resid;   // nullable
+    const void* weight;  // nullable
+    void* h;             // nullable
+    void* y;             // nullable
+    int8_t* q;           // nullable
+    float* q_scale;
 };
 
 struct CombineArgs {
@@ -315,6 +367,8 @@ hipError_t launch_shared_gate(const void* x, const void* w_sg, int32_t T, int32_
                               hipStream_t s);
 hipError_t launch_expert_ffn_fetched(const FfnArgs& a, const FetchArgs& f, hipStream_t s);
 hipError_t launch_combine(const CombineArgs& a, hipStream_t s);
+hipError_t launch_expert_ffn_i8(const FfnI8Args& a, hipStream_t s);
+hipError_t launch_rmsnorm_quant(const NormArgs& a, hipStream_t s);
 hipError_t launch_spec_update(const SpecArgs& a, hipStream_t s);
 
 // LoRE calibration fit (lore_fit.hip).

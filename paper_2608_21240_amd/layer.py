@@ -11,6 +11,10 @@ runs the path in the order the paper describes (Sec. 4.3):
              a ready word)  ........................................ -> combine (reads resid over PCIe)
     host   :   wait(ready word) -> exact residual on CPU threads -> resid (pinned) ^
 
+8-bit experts (wfmt INT8) take their activations from the norm in front of the layer
+(LayerRun.norm: residual addition, RMS norm, 8-bit rows with a scale per token), and a scoring
+rule (score=) another routing; both run as the separate calls.
+
 With layer_call=False the same layer runs as the separate calls (moe_route_bucket,
 moe_expert_ffn_grouped, moe_combine) and the host waits for the routing call's event.
 
@@ -27,7 +31,7 @@ import numpy as np
 import torch
 
 from . import spice, synth
-from .workloads import DTYPE_BF16, WFMT_MXFP4, Workload
+from .workloads import DTYPE_BF16, WFMT_INT8, WFMT_MXFP4, Workload
 
 
 def torch_dtype(dtype: int) -> torch.dtype:
@@ -114,16 +118,20 @@ class DeviceLayer:
         td = torch_dtype(dt)
         self.wg = to_tensor(host.wg, dt, device)
         self.bias = None if host.bias is None else torch.from_numpy(host.bias).to(device)
-        self.w13s = to_tensor(host.w13s, dt, device)
-        self.w2s = to_tensor(host.w2s, dt, device)
+        self.wfmt = host.wl.wfmt
+        if self.wfmt == WFMT_INT8:
+            self.w13s, self.w2s = self._weights(host.w13s).to(device), self._weights(host.w2s).to(device)
+        else:
+            self.w13s = to_tensor(host.w13s, dt, device)
+            self.w2s = to_tensor(host.w2s, dt, device)
         self.w_sg = None if host.w_sg is None else to_tensor(host.w_sg, dt, device)
         slot = np.full(s.n_experts, -1, np.int32)
         host.prefetch(range(s.n_experts) if host_exact else host.resident,
                       range(s.n_experts) if s.lore_rank > 0 else ())
-        self.wfmt = host.wl.wfmt
-        if self.wfmt == WFMT_MXFP4:
-            # one MXFP4 byte blob per slot: [2I][d] and [d][I] (codes, then block scales)
-            b13, b2 = synth.mxfp4_bytes(2 * s.inter, s.d), synth.mxfp4_bytes(s.d, s.inter)
+        if self.wfmt in (WFMT_MXFP4, WFMT_INT8):
+            # one byte blob per slot: [2I][d] and [d][I] (codes, then block or row scales)
+            blob = synth.mxfp4_bytes if self.wfmt == WFMT_MXFP4 else synth.int8_bytes
+            b13, b2 = blob(2 * s.inter, s.d), blob(s.d, s.inter)
             self.w13_pool = torch.empty((max(self.C, 1), b13), dtype=torch.uint8, device=device)
             self.w2_pool = torch.empty((max(self.C, 1), b2), dtype=torch.uint8, device=device)
         else:
@@ -155,8 +163,8 @@ class DeviceLayer:
                     self.host_w2[e] = self._weights(w2, pin=True)
 
     def _weights(self, a: np.ndarray, pin: bool = False) -> torch.Tensor:
-        """A routed expert's weight array (storage dtype, or an MXFP4 byte blob) as a tensor."""
-        if self.wfmt == WFMT_MXFP4:
+        """A weight array (storage dtype, or a byte blob) as a tensor."""
+        if self.wfmt in (WFMT_MXFP4, WFMT_INT8):
             t = torch.from_numpy(np.ascontiguousarray(a, dtype=np.uint8))
             return t.pin_memory() if pin else t
         return to_tensor(a, self.shape.dtype, pin=pin)
@@ -167,13 +175,15 @@ class DeviceLayer:
 
 
 class LayerRun:
-    """Buffers and streams for layer calls with up to T tokens."""
+    """Buffers and streams for layer calls with up to T tokens.  score: a spice.route_score() rule for
+    the routing; with it, and with 8-bit experts, the layer runs as separate calls."""
 
     def __init__(self, shape, T: int, n_slots: int, tau: float = 0.5, conf_mode: int = 0, norm_topk: int = 0,
                  device: str = "cuda", keep_logits: bool = False, fetch_slots: int = 0, wfmt: int = 0,
-                 layer_call: bool = True):
+                 layer_call: bool = True, score=None):
         self.shape, self.T = shape, T
-        self.layer_call = layer_call
+        self.score = score
+        self.layer_call = layer_call and score is None and wfmt != WFMT_INT8
         self.cfg = spice.make_cfg(shape, n_slots, tau, conf_mode, norm_topk, wfmt)
         s, K, N, d = shape, shape.top_k, shape.n_experts, shape.d
         i32 = dict(dtype=torch.int32, device=device)
@@ -192,6 +202,11 @@ class LayerRun:
         if self.ws_bytes == 0:
             raise ValueError(f"invalid configuration for the library: {spice.last_error()}")
         self.ws = torch.zeros(self.ws_bytes, dtype=torch.uint8, device=device)
+        # what the norm in front of the layer leaves: residual stream, normed rows, 8-bit rows and their scales
+        self.h = self.y = self.x_q = self.x_scale = None
+        if wfmt == WFMT_INT8:
+            self.x_q = torch.empty((T, d), dtype=torch.int8, device=device)
+            self.x_scale = torch.empty(T, **f32)
         # pinned host memory of the exact CPU path: the route kernel writes x and the
         # routing here, the CPU writes the residual that the combine kernel reads
         self.x_host = torch.empty((T, d), dtype=torch_dtype(s.dtype)).pin_memory()
@@ -228,15 +243,29 @@ class LayerRun:
             raise ValueError(f"the layer's expert weights are in format {L.wfmt}, the run was made for {self.cfg.wfmt}")
 
     # -- the steps, each one C-ABI call ------------------------------------------------
+    def norm(self, x: torch.Tensor, resid: Optional[torch.Tensor], weight: Optional[torch.Tensor], eps: float,
+             T: Optional[int] = None) -> torch.Tensor:
+        """The norm in front of the layer: self.h = x + resid, the normed rows self.y (returned: the layer's
+        input) and, for 8-bit experts, self.x_q with self.x_scale."""
+        T = self.T if T is None else T
+        if self.y is None:
+            self.h = torch.empty((self.T, self.shape.d), dtype=torch_dtype(self.shape.dtype), device=x.device)
+            self.y = torch.empty_like(self.h)
+        spice.moe_rmsnorm_quant(self.cfg, T, x, resid, weight, eps, self.h, self.y, self.x_q, self.x_scale)
+        return self.y
+
     def route(self, L: DeviceLayer, x: torch.Tensor, conf: Optional[torch.Tensor], T: Optional[int] = None,
               to_host: bool = True, mark: bool = True):
         """Routing + bucketing; with to_host the kernel also fills the pinned host copies.
         e_route marks the end of the call on the stream (mark=False records no event, for
         back-to-back timing; the host then has nothing to wait on)."""
         T = self.T if T is None else T
-        spice.moe_route_bucket(self.cfg, T, x, L.wg, L.bias, L.resident_slot, conf, self.logits, self.topk_idx,
-                               self.topk_w, self.slot_class, self.offsets, self.perm, self.inv_perm,
-                               self.host_out_ev if to_host else None, self.ws, self.ws_bytes)
+        args = (T, x, L.wg, L.bias, L.resident_slot, conf, self.logits, self.topk_idx, self.topk_w, self.slot_class,
+                self.offsets, self.perm, self.inv_perm, self.host_out_ev if to_host else None, self.ws, self.ws_bytes)
+        if self.score is None:
+            spice.moe_route_bucket(self.cfg, *args)
+        else:
+            spice.moe_route_bucket_scored(self.cfg, self.score, *args)
         if mark:
             self.e_route.record(torch.cuda.current_stream())
         self.wait_ready = False
@@ -250,6 +279,8 @@ class LayerRun:
         T = self.T if T is None else T
         ho = None
         self._same_format(L)
+        if self.score is not None:
+            raise ValueError("a scoring rule takes the separate calls (route, experts, combine)")
         if to_host:
             self.epoch = (self.epoch + 1) & 0x7FFFFFFF
             self.host_out.ready_value = self.epoch
@@ -267,7 +298,11 @@ class LayerRun:
         T = self.T if T is None else T
         self._same_format(L)
         la, lb = (L.lore_A, L.lore_B) if fuse_lore else (None, None)
-        if L.w_sg is not None:
+        if self.cfg.wfmt == WFMT_INT8:
+            spice.moe_expert_ffn_grouped_i8(self.cfg, T, self.x_q, self.x_scale, x, self.perm, self.offsets,
+                                            L.resident_slot, L.w13_pool, L.w2_pool, L.w13s, L.w2s, L.w_sg, la, lb,
+                                            self.y_slots, self.y_shared, self.ws, self.ws_bytes)
+        elif L.w_sg is not None:
             spice.moe_expert_ffn_grouped_gated(self.cfg, T, x, self.perm, self.offsets, L.resident_slot, L.w13_pool,
                                                L.w2_pool, L.w13s, L.w2s, L.w_sg, la, lb, self.y_slots,
                                                self.y_shared, self.ws, self.ws_bytes)
@@ -323,17 +358,23 @@ class LayerRun:
 
     def forward(self, L: DeviceLayer, x: torch.Tensor, conf: Optional[torch.Tensor], T: Optional[int] = None,
                 exact: bool = True, n_threads: int = 0, events: Optional[Dict[str, torch.cuda.Event]] = None,
-                split=None, after_experts=None, before_residual=None):
+                split=None, after_experts=None, before_residual=None, norm=None):
         """One layer call: route, FFN + LoRE on the GPU overlapped with the exact CPU residual
         (and, with a split cost model, the fetched exact misses on the GPU), combine.
         after_experts (callable) queues more GPU work right after the FFN, ahead of the host
         residual, e.g. a speculative-prefetch rollout; before_residual (callable) runs on the
-        host once the routing's host copies are there, just before the residual."""
+        host once the routing's host copies are there, just before the residual.  norm: (residual or None,
+        weight or None, eps) runs the norm on x first, and its rows are the layer's input (8-bit experts need
+        it: it gives them their activations)."""
         T = self.T if T is None else T
         ev = events or {}
-        self.x_cur = x
+        if norm is None and self.cfg.wfmt == WFMT_INT8:
+            raise ValueError("8-bit experts take their activations from the norm: pass norm=(residual, weight, eps)")
         if "start" in ev:
             ev["start"].record()
+        if norm is not None:
+            x = self.norm(x, *norm, T=T)
+        self.x_cur = x
         if self.layer_call:
             self.layer_gpu(L, x, conf, T, to_host=exact)
         else:

@@ -19,7 +19,8 @@ SPICE_OK, SPICE_ERR_INVALID, SPICE_ERR_UNSUPPORTED, SPICE_ERR_HIP, SPICE_ERR_WOR
     0, -1, -2, -3, -4, -5)
 SPICE_F32, SPICE_BF16 = 0, 1
 SPICE_CONF_INPUT, SPICE_CONF_GATE, SPICE_CONF_GATE_RENORM = 0, 1, 2
-SPICE_WFMT_DTYPE, SPICE_WFMT_MXFP4 = 0, 2
+SPICE_WFMT_DTYPE, SPICE_WFMT_MXFP4, SPICE_WFMT_INT8 = 0, 2, 3
+SPICE_SCORE_SOFTMAX, SPICE_SCORE_SIGMOID = 0, 1
 SPICE_CLASS_HIT, SPICE_CLASS_LORE, SPICE_CLASS_EXACT, SPICE_CLASS_EXACT_GPU = 0, 1, 2, 3
 SPICE_MAX_EXPERTS, SPICE_MAX_TOKENS, SPICE_MAX_LORE_RANK = 256, 65536, 256
 SPICE_WS_CONTROL_BYTES = 131072
@@ -29,6 +30,7 @@ SPICE_FLAG_BAD_SLOT, SPICE_FLAG_BAD_INDEX = 1, 2
 EXPORTS = (
     "spice_workspace_bytes", "spice_workspace_init", "spice_workspace_flags",
     "moe_route_bucket", "moe_expert_ffn_grouped", "moe_expert_ffn_grouped_gated", "lore_surrogate_apply",
+    "moe_route_bucket_scored", "moe_rmsnorm_quant", "moe_expert_ffn_grouped_i8",
     "moe_combine", "moe_layer_gpu", "moe_layer_gpu_noalloc",
     "moe_exact_residual_host", "moe_cache_create", "moe_cache_step", "moe_cache_wait", "moe_cache_state",
     "moe_cache_destroy", "moe_split_plan", "moe_fetch_experts", "moe_expert_ffn_fetched",
@@ -57,6 +59,11 @@ class spice_split_cost_t(ctypes.Structure):
                 ("margin", ctypes.c_double)]
 
 
+class spice_route_score_t(ctypes.Structure):
+    _fields_ = [("score", ctypes.c_int32), ("n_group", ctypes.c_int32), ("topk_group", ctypes.c_int32),
+                ("group_top", ctypes.c_int32), ("scale", ctypes.c_float), ("balance_bias", ctypes.c_void_p)]
+
+
 class spice_spec_host_t(ctypes.Structure):
     _fields_ = [("pred_idx", ctypes.c_void_p), ("pred_prob", ctypes.c_void_p), ("conf", ctypes.c_void_p)]
 
@@ -72,6 +79,14 @@ def host_out(x=None, topk_idx=None, topk_w=None, slot_class=None, class_counts=N
     """Pinned host buffers (tensors, arrays or addresses) for the routing's host copies."""
     return spice_host_out_t(_p(x), _p(topk_idx), _p(topk_w), _p(slot_class), _p(class_counts), _p(ready),
                             ready_value & 0xFFFFFFFF)
+
+
+def route_score(score: int = SPICE_SCORE_SOFTMAX, n_group: int = 1, topk_group: int = 1, group_top: int = 1,
+                scale: float = 1.0, balance_bias=None) -> spice_route_score_t:
+    """Scoring rule of moe_route_bucket_scored (balance_bias: device fp32 [N], which the struct keeps alive)."""
+    s = spice_route_score_t(score, n_group, topk_group, group_top, scale, _p(balance_bias))
+    s.keep = balance_bias
+    return s
 
 
 def make_cfg(shape, n_slots: int, tau: float = 0.5, conf_mode: int = SPICE_CONF_INPUT,
@@ -97,6 +112,10 @@ def lib() -> ctypes.CDLL:
             "spice_workspace_flags": (_I, [_P, _Z, ctypes.POINTER(ctypes.c_uint32), _I, _P]),
             "moe_route_bucket": (_I, [C, _I, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P,
                                       ctypes.POINTER(spice_host_out_t), _P, _Z, _P]),
+            "moe_route_bucket_scored": (_I, [C, ctypes.POINTER(spice_route_score_t), _I, _P, _P, _P, _P, _P, _P, _P,
+                                             _P, _P, _P, _P, _P, ctypes.POINTER(spice_host_out_t), _P, _Z, _P]),
+            "moe_rmsnorm_quant": (_I, [C, _I, _P, _P, _P, ctypes.c_float, _P, _P, _P, _P, _P]),
+            "moe_expert_ffn_grouped_i8": (_I, [C, _I] + [_P] * 16 + [_Z, _P]),
             "moe_expert_ffn_grouped": (_I, [C, _I, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _Z, _P]),
             "moe_expert_ffn_grouped_gated": (_I, [C, _I, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _Z,
                                                   _P]),
@@ -166,7 +185,9 @@ def _check(fn: str, st: int) -> None:
 
 def _matrix_bytes(cfg, rows: int, K: int) -> int:
     """Bytes of one routed-expert matrix [rows][K] in the cfg's weight format (the MXFP4 blob
-    holds rows*K/2 code bytes and rows*K/32 scale bytes)."""
+    holds rows*K/2 code bytes and rows*K/32 scale bytes, the 8-bit one rows*K codes and rows fp32 scales)."""
+    if cfg.wfmt == SPICE_WFMT_INT8:
+        return rows * K + 4 * rows
     if cfg.wfmt == SPICE_WFMT_MXFP4:
         return rows * K // 2 + rows * K // 32
     return rows * K * (2 if cfg.dtype == SPICE_BF16 else 4)
@@ -221,6 +242,31 @@ def moe_route_bucket(cfg, T, x, w_gate, logit_bias, resident_slot, conf, logits,
         ctypes.byref(cfg), T, _p(x), _p(w_gate), _p(logit_bias), _p(resident_slot), _p(conf), _p(logits),
         _p(topk_idx), _p(topk_w), _p(slot_class), _p(offsets), _p(perm), _p(inv_perm),
         None if host_out is None else ctypes.byref(host_out), _p(ws), ws_bytes, _stream(stream)))
+
+
+def moe_route_bucket_scored(cfg, score: spice_route_score_t, T, x, w_gate, logit_bias, resident_slot, conf, logits,
+                            topk_idx, topk_w, slot_class, offsets, perm, inv_perm,
+                            host_out: Optional[spice_host_out_t], ws, ws_bytes, stream=None) -> None:
+    _check("moe_route_bucket_scored", lib().moe_route_bucket_scored(
+        ctypes.byref(cfg), ctypes.byref(score), T, _p(x), _p(w_gate), _p(logit_bias), _p(resident_slot), _p(conf),
+        _p(logits), _p(topk_idx), _p(topk_w), _p(slot_class), _p(offsets), _p(perm), _p(inv_perm),
+        None if host_out is None else ctypes.byref(host_out), _p(ws), ws_bytes, _stream(stream)))
+
+
+def moe_rmsnorm_quant(cfg, T, x, resid, weight, eps, h_out, y_out, q_out, q_scale, stream=None) -> None:
+    _check("moe_rmsnorm_quant", lib().moe_rmsnorm_quant(
+        ctypes.byref(cfg), T, _p(x), _p(resid), _p(weight), eps, _p(h_out), _p(y_out), _p(q_out), _p(q_scale),
+        _stream(stream)))
+
+
+def moe_expert_ffn_grouped_i8(cfg, T, x_q, x_scale, x, perm, offsets, resident_slot, w13_pool, w2_pool, w13_shared,
+                              w2_shared, w_shared_gate, lore_A, lore_B, y_slots, y_shared, ws, ws_bytes,
+                              stream=None) -> None:
+    _check_pools("moe_expert_ffn_grouped_i8", cfg, w13_pool, w2_pool)
+    _check("moe_expert_ffn_grouped_i8", lib().moe_expert_ffn_grouped_i8(
+        ctypes.byref(cfg), T, _p(x_q), _p(x_scale), _p(x), _p(perm), _p(offsets), _p(resident_slot), _p(w13_pool),
+        _p(w2_pool), _p(w13_shared), _p(w2_shared), _p(w_shared_gate), _p(lore_A), _p(lore_B), _p(y_slots),
+        _p(y_shared), _p(ws), ws_bytes, _stream(stream)))
 
 
 def moe_expert_ffn_grouped(cfg, T, x, perm, offsets, resident_slot, w13_pool, w2_pool, w13_shared, w2_shared,

@@ -23,7 +23,7 @@ from typing import List, Optional, Tuple
 
 import numpy as np
 
-from .workloads import DTYPE_BF16, DTYPE_F32, WFMT_MXFP4, Workload
+from .workloads import DTYPE_BF16, DTYPE_F32, WFMT_INT8, WFMT_MXFP4, Workload
 
 WEIGHT_STD = 0.02
 
@@ -165,22 +165,43 @@ def mxfp4_bytes(rows: int, K: int) -> int:
     return rows * K // 2 + rows * K // 32
 
 
+def quantize_int8(a: np.ndarray) -> np.ndarray:
+    """A [rows][K] fp32 matrix -> one 8-bit byte blob: rows*K int8 codes row-major, then rows fp32
+    scales max |a| / 127; codes go to the nearest integer, ties to even.  A row of zeros gets scale 0."""
+    a = np.asarray(a, np.float64)
+    scale = (np.abs(a).max(axis=1) / 127).astype(np.float32)
+    div = np.where(scale > 0, scale, 1).astype(np.float64)
+    codes = np.clip(np.rint(a / div[:, None]), -127, 127).astype(np.int8)
+    return np.concatenate([codes.reshape(-1).view(np.uint8), scale.view(np.uint8)])
+
+
+def int8_bytes(rows: int, K: int) -> int:
+    return rows * K + 4 * rows
+
+
 def gen_expert(wl: Workload, layer: int, e: int) -> Tuple[np.ndarray, np.ndarray]:
     """Routed expert e: w13[2I][d] (rows 0..I-1 gate W1, rows I..2I-1 up W3), w2[d][I] in the
-    storage dtype, or as MXFP4 blobs (quantize_mxfp4 of the same draws) when wl.wfmt is MXFP4."""
+    storage dtype, or as MXFP4 or 8-bit blobs (quantize_mxfp4 / quantize_int8 of the same draws) by wl.wfmt."""
     s = wl.shape
-    if wl.wfmt == WFMT_MXFP4:
+    if wl.wfmt in (WFMT_MXFP4, WFMT_INT8):
+        quantize = quantize_mxfp4 if wl.wfmt == WFMT_MXFP4 else quantize_int8
         w13 = rng(*_key(wl, layer, T_W13, e)).standard_normal(size=(2 * s.inter, s.d), dtype=np.float32)
         w2 = rng(*_key(wl, layer, T_W2, e)).standard_normal(size=(s.d, s.inter), dtype=np.float32)
-        return quantize_mxfp4(w13 * np.float32(WEIGHT_STD)), quantize_mxfp4(w2 * np.float32(WEIGHT_STD))
+        return quantize(w13 * np.float32(WEIGHT_STD)), quantize(w2 * np.float32(WEIGHT_STD))
     w13 = _normal(_key(wl, layer, T_W13, e), (2 * s.inter, s.d), WEIGHT_STD, s.dtype)
     w2 = _normal(_key(wl, layer, T_W2, e), (s.d, s.inter), WEIGHT_STD, s.dtype)
     return w13, w2
 
 
 def gen_shared(wl: Workload, layer: int = 0) -> Tuple[np.ndarray, np.ndarray]:
-    """Shared block: w13s[2 I_s][d], w2s[d][I_s]."""
+    """Shared block: w13s[2 I_s][d], w2s[d][I_s] (8-bit blobs of the same draws when wl.wfmt is INT8)."""
     s = wl.shape
+    if wl.wfmt == WFMT_INT8:
+        w13 = rng(*_key(wl, layer, T_W13S)).standard_normal(size=(2 * s.shared_inter, s.d), dtype=np.float32)
+        w2 = rng(*_key(wl, layer, T_W2S)).standard_normal(size=(s.d, s.shared_inter), dtype=np.float32)
+        if s.shared_inter == 0:
+            return np.empty(0, np.uint8), np.empty(0, np.uint8)
+        return quantize_int8(w13 * np.float32(WEIGHT_STD)), quantize_int8(w2 * np.float32(WEIGHT_STD))
     w13 = _normal(_key(wl, layer, T_W13S), (2 * s.shared_inter, s.d), WEIGHT_STD, s.dtype)
     w2 = _normal(_key(wl, layer, T_W2S), (s.d, s.shared_inter), WEIGHT_STD, s.dtype)
     return w13, w2

@@ -1,0 +1,182 @@
+"""The 8-bit MoE block without a GPU: what its entry points refuse, its weight format in the host's
+residual, the cache and the layer generator."""
+import ctypes
+
+import numpy as np
+import pytest
+
+from paper_2608_21240_amd import spice, synth, workloads as W
+
+D = 0x100000  # never dereferenced: every call below fails validation first
+INVALID, UNSUPPORTED = spice.SPICE_ERR_INVALID, spice.SPICE_ERR_UNSUPPORTED
+S = W.MoEShape(d=256, n_experts=16, top_k=4, inter=96, shared_inter=160, lore_rank=8, dtype=W.DTYPE_BF16)
+
+
+def cfg(shape=S, **kw):
+    c = spice.make_cfg(shape, n_slots=kw.pop("n_slots", 5), wfmt=kw.pop("wfmt", spice.SPICE_WFMT_INT8))
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return c
+
+
+def norm(c=None, T=4, x=D, resid=2 * D, weight=3 * D, eps=1e-6, h=4 * D, y=5 * D, q=6 * D, qs=7 * D):
+    return spice.lib().moe_rmsnorm_quant(ctypes.byref(cfg() if c is None else c), T, x, resid, weight, eps, h, y, q, qs, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(x=None), INVALID), (dict(h=None, y=None, q=None, qs=None), INVALID), (dict(q=None), INVALID),
+    (dict(qs=None), INVALID), (dict(eps=-1.0), INVALID), (dict(eps=float("nan")), INVALID),
+    (dict(eps=float("inf")), INVALID), (dict(T=-1), INVALID), (dict(T=65537), UNSUPPORTED),
+    (dict(h=D + 256), INVALID), (dict(y=2 * D - 16), INVALID), (dict(q=D), INVALID), (dict(q=D + 64), INVALID),
+    (dict(h=5 * D), INVALID), (dict(qs=6 * D + 128), INVALID), (dict(y=3 * D), INVALID), (dict(h=D, y=D), INVALID),
+    (dict(x=D + 8), UNSUPPORTED), (dict(q=6 * D + 8), UNSUPPORTED), (dict(qs=7 * D + 2), UNSUPPORTED),
+    (dict(weight=3 * D + 4), UNSUPPORTED)])
+def test_norm_refuses(kw, status):
+    assert norm(**kw) == status
+    assert spice.last_error()
+
+
+def test_no_tokens_are_no_work():
+    assert norm(T=0, x=None, h=None, y=None, q=None, qs=None) == spice.SPICE_OK
+    assert ffn(T=0, x_q=None, ws=None) == spice.SPICE_OK
+    assert route(T=0) == spice.SPICE_OK
+
+
+def route(T=4, c=None, null=False, **kw):
+    c = cfg() if c is None else c
+    sc = spice.route_score(**kw)
+    ws = spice.spice_workspace_bytes(c, max(T, 1))
+    return spice.lib().moe_route_bucket_scored(ctypes.byref(c), None if null else ctypes.byref(sc), T, D, D, None, D,
+                                               D, None, D, D, D, D, D, D, None, D, ws, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(score=2), INVALID), (dict(score=-1), INVALID), (dict(n_group=0), INVALID), (dict(n_group=3), INVALID),
+    (dict(n_group=-4), INVALID), (dict(n_group=4, topk_group=0), INVALID), (dict(n_group=4, topk_group=5), INVALID),
+    (dict(n_group=8, topk_group=1), INVALID),  # 2 experts kept for top-4
+    (dict(group_top=0), INVALID), (dict(group_top=3), INVALID), (dict(scale=float("nan")), INVALID),
+    (dict(scale=float("inf")), INVALID), (dict(null=True), INVALID)])
+def test_scored_routing_refuses(kw, status):
+    assert route(**kw) == status
+    assert spice.last_error()
+
+
+def test_scored_routing_takes_at_most_64_groups():
+    wide = cfg(W.MoEShape(256, 130, 2, 96, 160, 8, W.DTYPE_BF16))
+    assert route(c=wide, n_group=65, topk_group=9) == UNSUPPORTED
+
+
+def ffn(T=4, c=None, ws_bytes=None, **kw):
+    c = cfg() if c is None else c
+    p = dict(x_q=D, x_scale=2 * D, x=3 * D, perm=D, offsets=D, resident_slot=D, w13_pool=D, w2_pool=D, w13_shared=D,
+             w2_shared=D, w_shared_gate=None, lore_A=None, lore_B=None, y_slots=16 * D, y_shared=32 * D, ws=D)
+    p.update(kw)
+    n = spice.spice_workspace_bytes(c, max(T, 1)) if ws_bytes is None else ws_bytes
+    return spice.lib().moe_expert_ffn_grouped_i8(ctypes.byref(c), T, *p.values(), n, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(x_q=None), INVALID), (dict(x_scale=None), INVALID), (dict(perm=None), INVALID), (dict(offsets=None), INVALID),
+    (dict(resident_slot=None), INVALID), (dict(w13_pool=None), INVALID), (dict(w2_shared=None), INVALID),
+    (dict(y_slots=None), INVALID), (dict(y_shared=None), INVALID), (dict(ws=None), INVALID),
+    (dict(x=None, w_shared_gate=D), INVALID), (dict(x=None, lore_A=D, lore_B=D), INVALID),
+    (dict(x_q=D + 8), UNSUPPORTED), (dict(w2_pool=D + 4), UNSUPPORTED), (dict(y_slots=D + 4), UNSUPPORTED),
+    (dict(y_slots=32 * D), INVALID), (dict(y_slots=D), INVALID), (dict(T=-1), INVALID),
+    (dict(ws_bytes=1 << 17), spice.SPICE_ERR_WORKSPACE), (dict(c=cfg(wfmt=0)), UNSUPPORTED),
+    (dict(c=cfg(W.MoEShape(256, 16, 4, 96, 160, 8, W.DTYPE_F32))), UNSUPPORTED),
+    (dict(c=cfg(W.MoEShape(264, 16, 4, 96, 160, 8, W.DTYPE_BF16))), UNSUPPORTED),
+    (dict(c=cfg(W.MoEShape(256, 16, 4, 104, 160, 8, W.DTYPE_BF16))), UNSUPPORTED),
+    (dict(c=cfg(W.MoEShape(256, 16, 4, 96, 168, 8, W.DTYPE_BF16))), UNSUPPORTED),
+    (dict(c=cfg(W.MoEShape(256, 16, 4, 131072, 160, 8, W.DTYPE_BF16))), UNSUPPORTED)])
+def test_experts_refuse(kw, status):
+    assert ffn(**kw) == status
+    assert spice.last_error()
+
+
+def test_calls_without_an_8_bit_form_refuse_it():
+    L, c = spice.lib(), cfg()
+    ws = spice.spice_workspace_bytes(c, 4)
+    assert ws > 0
+    assert L.moe_expert_ffn_grouped(ctypes.byref(c), 4, *[D] * 8, None, None, 16 * D, 32 * D, D, ws, None) == UNSUPPORTED
+    assert "moe_expert_ffn_grouped_i8" in spice.last_error()
+    assert L.moe_layer_gpu(ctypes.byref(c), 4, *[D] * 9, None, None, None, None, *[D] * 6, 16 * D, 32 * D, None, None,
+                           None, D, ws, None) == UNSUPPORTED
+    assert L.moe_expert_ffn_fetched(ctypes.byref(c), 4, *[D] * 7, 2, 16 * D, D, ws, None) == UNSUPPORTED
+    assert L.moe_lore_fit(ctypes.byref(c), 8, 4, *[D] * 7, None, None, D, 1 << 30, None) == UNSUPPORTED
+    assert spice.spice_workspace_bytes(cfg(wfmt=1), 4) == 0
+
+
+def test_short_8_bit_pools_are_rejected_by_the_binding():
+    import torch
+
+    p13, p2 = (torch.empty((5, synth.int8_bytes(*s)), dtype=torch.uint8) for s in ((192, 256), (256, 96)))
+    spice._check_pools("t", cfg(), p13, p2)
+    with pytest.raises(ValueError, match="w2_pool"):
+        spice._check_pools("t", cfg(), p13, p2[:4])
+
+
+def decode(b, rows, k):
+    return b[: rows * k].view(np.int8).reshape(rows, k) * b[rows * k:].view(np.float32).astype(np.float64)[:, None]
+
+
+def test_quantize_int8():
+    a = np.random.default_rng(1).standard_normal((7, 48)).astype(np.float32)
+    a[3] = 0
+    b = synth.quantize_int8(a)
+    assert b.size == synth.int8_bytes(7, 48)
+    step = np.abs(a).max(1, keepdims=True) / 127
+    # half a code, plus the scale's rounding (2^-24) on up to 127 codes
+    assert (np.abs(decode(b, 7, 48) - a) <= step * (0.5 + 127 * 2.0 ** -23)).all()
+    assert (decode(b, 7, 48)[3] == 0).all()
+
+
+@pytest.mark.parametrize("shape,T", [(S, 5), (W.MoEShape(48, 6, 3, 16, 0, 0, W.DTYPE_BF16), 11), (S, 1)])
+def test_host_residual_of_8_bit_experts(shape, T):
+    """Activations stay fp32 on the host: fp32 sums over exact products, 3 d and 3 I roundings at most."""
+    s, N, K = shape, shape.n_experts, shape.top_k
+    wl = W.Workload("t", s, tokens=T, resident=0, skew=False, wfmt=W.WFMT_INT8)
+    r = np.random.default_rng(5)
+    idx = np.stack([r.permutation(N)[:K] for _ in range(T)]).astype(np.int32)
+    cls = r.integers(0, 3, (T, K)).astype(np.uint8)
+    w = r.random((T, K)).astype(np.float32)
+    x = synth.gen_x(wl)
+    w13, w2 = zip(*[synth.gen_expert(wl, 0, e) for e in range(N)])
+    out = np.full((T, s.d), np.nan, np.float32)
+    spice.moe_exact_residual_host(spice.make_cfg(s, 0, wfmt=W.WFMT_INT8), T, x, idx, w, cls, w13, w2, out, 3)
+    xf = synth.bf16_bits_to_f32(x).astype(np.float64)
+    for t in range(T):
+        ref, room = np.zeros(s.d), np.zeros(s.d)
+        for k in range(K):
+            if cls[t, k] != 2:
+                continue
+            a, b = decode(w13[idx[t, k]], 2 * s.inter, s.d), decode(w2[idx[t, k]], s.d, s.inter)
+            g, u = a[: s.inter] @ xf[t], a[s.inter:] @ xf[t]
+            eg = np.abs(a) @ np.abs(xf[t]) * (s.d + 4) * 2.0 ** -24
+            h = g / (1 + np.exp(-g)) * u
+            # |silu'| <= 1.1, and a few roundings of silu and the product
+            eh = 1.1 * eg[: s.inter] * np.abs(u) + np.abs(g) * eg[s.inter:] + np.abs(h) * (16 + np.abs(g)) * 2.0 ** -24
+            ref += w[t, k] * (b @ h)
+            room += w[t, k] * (np.abs(b) @ (eh + np.abs(h) * (s.inter + 8) * 2.0 ** -24))
+        assert (np.abs(out[t] - ref) <= room).all()
+
+
+def test_cache_copies_whole_8_bit_blobs():
+    """The cache's bookkeeping takes the format (copies need a GPU: the layer test there)."""
+    c = spice.ExpertCache(cfg(), 1, [[0, 1, 2, 3, 4]])
+    adm, ev = c.step(0, 0, np.array([[7, 8, 0, 1]], np.int32), np.array([[2, 1, 0, 0]], np.uint8), 4)
+    assert (adm, ev) == ([7], [2])
+    c.close()
+
+
+def test_layer_driver_asks_for_the_norm():
+    pytest.importorskip("torch")
+    from paper_2608_21240_amd import layer as LY
+
+    run = LY.LayerRun.__new__(LY.LayerRun)
+    run.T, run.cfg = 4, cfg()
+    with pytest.raises(ValueError, match="norm"):
+        run.forward(None, None, None)
+    run.score, run.cfg = spice.route_score(), cfg(wfmt=0)
+    run.shape = S
+    with pytest.raises(ValueError, match="separate calls"):
+        run.layer_gpu(type("L", (), {"wfmt": 0})(), None, None)
