@@ -267,10 +267,14 @@ hipError_t launch_expert_ffn_i8(const FfnI8Args& a, hipStream_t s) {
     const long long rows = (a.Is > 0 ? a.T : 0) + (a.C > 0 ? (long long)a.T * a.K : 0);
     if (rows == 0) return hipSuccess;
     if (std::max({up, down, rows}) > 0x7FFFFFFFll) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(i8_up_kernel, dim3((unsigned)up), dim3(kThreads), 0, s, a);
+    const bool gemm = expert_gemm_i8_applies(a);
+    hipError_t e = hipSuccess;
+    if (gemm) e = launch_expert_gemm_i8(a, true, s);
+    else hipLaunchKernelGGL(i8_up_kernel, dim3((unsigned)up), dim3(kThreads), 0, s, a);
     hipLaunchKernelGGL(i8_quant_kernel, dim3((unsigned)rows), dim3(kThreads), 0, s, a);
-    hipLaunchKernelGGL(i8_down_kernel, dim3((unsigned)down), dim3(kThreads), 0, s, a);
-    return hipGetLastError();
+    if (e == hipSuccess && gemm) e = launch_expert_gemm_i8(a, false, s);
+    else if (!gemm) hipLaunchKernelGGL(i8_down_kernel, dim3((unsigned)down), dim3(kThreads), 0, s, a);
+    return e == hipSuccess ? hipGetLastError() : e;
 }
 
 }  // namespace spice

@@ -1,0 +1,466 @@
+// The 8-bit expert FFN's products as GEMM tiles, for many tokens (expert_ffn_i8.hip has the operator's
+// three steps and the streaming tiles that take fewer tokens).
+//
+//   up   : H[pos][f] = silu(sx s1[f] sum_k W1[f][k] x[k]) * (sx s3[f] sum_k W3[f][k] x[k])  (fp32)
+//   down : Y[pos][j] = sh s2[j] sum_k W2[j][k] qh[k]                                         (fp32)
+//
+// A block computes BM weight rows x BT tokens over the whole contraction, 128 k per stage
+// (v_mfma_i32_16x16x64_i8, weights as the A operand, tokens as B).  For `up` the rows are BM / 2 W1 rows
+// and the same W3 rows, so a wave holds the gate and up sums of its features and applies the scales and
+// SwiGLU in registers.  A wave's token sub-tiles are interleaved with the other waves' (rows kTStride t +
+// 16 wt), so the ragged last tile of an expert spreads over the SIMDs; sub-tiles without a live token are
+// not read and issue no MFMA, and their rows are not fetched.
+//
+// Staging: buffer loads straight to LDS into a ring of S stages of 128-byte rows whose 16-byte chunks are
+// XOR-swizzled by row (chunk c of row r at c ^ ((r >> 1) & 7)).  A chunk past the end of a row, and a row
+// past the end of a matrix or a bucket, reads zero (an offset past the buffer).
+// Pipeline: the fragments of a stage's two k-steps are read half a stage ahead of their MFMAs; one barrier
+// per stage, in the middle of the MFMAs, frees the buffer just read for the stage S ahead.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "spice_internal.h"
+
+namespace spice {
+namespace {
+
+template <int BM_, int BT_, int WF_, int WT_, int S_, int L_>
+struct Shape {
+    static constexpr int BM = BM_, BT = BT_, WF = WF_, WT = WT_, S = S_;
+    static constexpr int kThreads = 64 * WF * WT;
+    static constexpr int kLoaders = 64 * L_;       // threads that issue the stages' loads
+    static constexpr int RF = BM / WF / 16;        // 16-row sub-tiles per wave
+    static constexpr int RT = BT / WT / 16;        // 16-token sub-tiles per wave
+    static constexpr int kTStride = 16 * WT;       // tile rows between a wave's token sub-tiles
+    static constexpr int kUpFeat = BM / 2;         // features of an up tile (W1 rows = W3 rows)
+    static constexpr int kWTile = BM * 128;        // bytes of a stage's weight rows
+    static constexpr int kStage = (BM + BT) * 128;
+    static constexpr int kRowStep = kLoaders / 8;  // rows one load instruction of the loaders covers
+    static constexpr int kWLoads = BM / kRowStep, kXLoads = BT / kRowStep;
+    static constexpr int kXcdBlocks = 32 * std::max(1, 163840 / (S * kStage));  // resident blocks per XCD
+    static_assert(kRowStep % 16 == 0 && kUpFeat % kRowStep == 0, "staged rows keep their swizzle");
+    static_assert(BM % kRowStep == 0 && BT % kRowStep == 0, "whole load instructions");
+    static_assert((S - 1) * (kWLoads + kXLoads) < 64, "vmcnt holds the loads in flight");
+};
+using Big = Shape<256, 256, 2, 4, 2, 4>;
+using Wide = Shape<256, 128, 4, 2, 3, 4>;
+using Small = Shape<128, 64, 2, 2, 3, 4>;
+
+constexpr int kBK = 128;                         // contraction per stage
+constexpr uint32_t kOutOfRange = 0xFFFFFFF0u;    // an offset past every buffer
+constexpr long long kMaxBuffer = 0xFFFF0000ll;   // bytes a buffer may hold
+constexpr int kRawBufferWord3 = 0x00020000;      // gfx9 raw buffer: 32-bit data format
+
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ float silu(float u) { return u / (1.0f + __expf(-u)); }
+
+// Logical tile of block b: rounds of 8 x per_xcd blocks give each XCD (block b runs on XCD b % 8) per_xcd
+// consecutive tiles, which share operands in that XCD's L2.  A bijection on [0, G).
+__device__ __forceinline__ int xcd_tile(int b, int G, int per_xcd) {
+    const int round = 8 * per_xcd;
+    if (b >= (G / round) * round) return b;
+    const int x = b & 7, slot = b >> 3;
+    return (slot / per_xcd) * round + x * per_xcd + slot % per_xcd;
+}
+
+struct Job {
+    FfnI8Args a;
+    int32_t super[2];  // shared-block super-tile (weight tiles, token tiles)
+};
+
+struct Tile {
+    bool shared;
+    const char* w;        // the matrix's blob
+    uint32_t w_bytes;     // of its codes
+    int kdim, nfeat;      // contraction, output features
+    int row0;             // first feature
+    int tok0, ntok;       // first token of the tile in its group, tokens of the group
+    int start;            // the group's first bucket position (0 for the shared block)
+};
+
+// The HIT bucket holding tile L of nt tiles per token tile, by a wave's scan of the offsets.
+__device__ bool find_bucket(const FfnI8Args& a, int nt, int BT, int& L, int lane, int& e_, int& st_, int& n_) {
+    const int32_t* off = a.offsets + SPICE_CLASS_HIT * (a.N + 1);
+    for (int e0 = 0; e0 < a.N; e0 += 64) {
+        const int e = e0 + lane;
+        int st = 0, n = 0;
+        if (e < a.N) {
+            st = off[e];
+            n = off[e + 1] - st;
+        }
+        if (n > a.T * a.K) n = 0;
+        const int tiles = n > 0 ? ((n + BT - 1) / BT) * nt : 0;
+        int incl = tiles;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int up = __shfl_up(incl, o);
+            if (lane >= o) incl += up;
+        }
+        const int excl = incl - tiles;
+        const unsigned long long hit = __ballot(tiles > 0 && L >= excl && L < incl);
+        if (hit) {
+            const int src = __builtin_amdgcn_readfirstlane(__ffsll((long long)hit) - 1);
+            e_ = e0 + src;
+            st_ = __builtin_amdgcn_readlane(st, src);
+            n_ = __builtin_amdgcn_readlane(n, src);
+            L -= __builtin_amdgcn_readlane(excl, src);
+            return true;
+        }
+        L -= __builtin_amdgcn_readlane(incl, 63);
+    }
+    return false;
+}
+
+// Logical tile L of a launch (every wave resolves it for itself): the shared block's tiles first, in
+// groups of about an XCD's blocks that share operand tiles in its L2, then the HIT buckets in id order,
+// the token tiles of one weight tile next to each other.
+template <bool kUp, class C>
+__device__ bool resolve(const Job& job, int L, Tile& j) {
+    const FfnI8Args& a = job.a;
+    constexpr int feat = kUp ? C::kUpFeat : C::BM;
+    const int nt_sh = ((kUp ? a.Is : a.d) + feat - 1) / feat, nt_e = ((kUp ? a.I : a.d) + feat - 1) / feat;
+    const int mt_sh = (a.T + C::BT - 1) / C::BT;
+    const int tiles_sh = a.Is > 0 ? nt_sh * mt_sh : 0;
+    if (L < tiles_sh) {
+        const int sn = job.super[0], sm = job.super[1];
+        const int g = L / (sn * sm), in = L - g * (sn * sm), mg = mt_sh / sm;
+        j.shared = true;
+        j.w = kUp ? a.w13s : a.w2s;
+        j.w_bytes = (uint32_t)(kUp ? 2 : 1) * (uint32_t)a.Is * (uint32_t)a.d;
+        j.kdim = kUp ? a.d : a.Is;
+        j.nfeat = kUp ? a.Is : a.d;
+        j.row0 = ((g / mg) * sn + in / sm) * feat;
+        j.tok0 = ((g % mg) * sm + in % sm) * C::BT;
+        j.ntok = a.T;
+        j.start = 0;
+        return true;
+    }
+    L -= tiles_sh;
+    int e = 0, st = 0, n = 0;
+    if (a.C <= 0 || !find_bucket(a, nt_e, C::BT, L, threadIdx.x & 63, e, st, n)) return false;
+    const int slot = a.resident_slot[e];
+    if (st < 0 || st + n > a.T * a.K || slot < 0 || slot >= a.C) {
+        if (threadIdx.x == 0)
+            atomicOr(&a.ctrl[kWordFlags], (uint32_t)(slot < 0 || slot >= a.C ? SPICE_FLAG_BAD_SLOT : SPICE_FLAG_BAD_INDEX));
+        return false;
+    }
+    const int mt = (n + C::BT - 1) / C::BT, nn = L / mt;
+    const size_t elems = (size_t)(kUp ? 2 : 1) * a.I * a.d, rows = kUp ? 2 * (size_t)a.I : (size_t)a.d;
+    j.shared = false;
+    j.w = (kUp ? a.w13_pool : a.w2_pool) + (size_t)slot * (elems + 4 * rows);
+    j.w_bytes = (uint32_t)elems;
+    j.kdim = kUp ? a.d : a.I;
+    j.nfeat = kUp ? a.I : a.d;
+    j.row0 = nn * feat;
+    j.tok0 = (L - nn * mt) * C::BT;
+    j.ntok = n;
+    j.start = st;
+    return true;
+}
+
+// Byte offset of 16-byte chunk c of staged row r inside an operand tile.
+__device__ __forceinline__ uint32_t lds_off(int r, int c) {
+    return (uint32_t)(r * 128 + ((c ^ ((r >> 1) & 7)) << 4));
+}
+
+typedef __amdgpu_buffer_rsrc_t rsrc_t;
+__device__ __forceinline__ rsrc_t raw_buffer(const void* p, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)bytes, kRawBufferWord3);
+}
+
+// 16 bytes from offset off of a buffer to LDS byte lds + 16 * lane, lds uniform over the wave (counted by
+// vmcnt; an offset past the buffer writes zeros).  Device pass only: the host pass of a kernel naming
+// this target builtin would lose its launch stub.
+__device__ __forceinline__ void load_lds16(rsrc_t b, uint32_t off, unsigned char* lds) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (__attribute__((address_space(3))) void*)lds, 16, (int)off, 0, 0, 0);
+#endif
+}
+
+// s_waitcnt with vmcnt(n) lgkmcnt(0), then the block's barrier: no wait for loads to LDS beyond those
+// the caller names (a __syncthreads would drain them all).
+template <int n>
+__device__ __forceinline__ void wait_and_barrier() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((n & 15) | ((n >> 4) << 14) | 0x70);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Fragments of one 64-k step: RF weight sub-tiles and the NL live token sub-tiles.
+template <class C, int NL>
+struct Frags {
+    i32x4_t a[C::RF], b[NL];
+};
+
+// The main loop of one tile with NL live token sub-tiles in this wave (NL = 0: the wave only loads and
+// keeps the barriers).
+template <class C, bool kUp, int NL, class Load>
+__device__ __forceinline__ void product(unsigned char* s_lds, int nk, uint32_t fbase, uint32_t tbase, Load load,
+                                        i32x4_t (&acc)[C::RF][C::RT]) {
+    constexpr int N1 = NL > 0 ? NL : 1;
+    constexpr int kLoads = (C::S - 2) * (C::kWLoads + C::kXLoads);  // stages in flight past the next one
+    auto read = [&](int buf, uint32_t kx, Frags<C, N1>& f) {
+        if constexpr (NL > 0) {
+            const unsigned char* base = s_lds + buf * C::kStage;
+#pragma unroll
+            for (int t = 0; t < NL; ++t)
+                f.b[t] = *reinterpret_cast<const i32x4_t*>(base + ((tbase + t * C::kTStride * 128) ^ kx));
+#pragma unroll
+            for (int s = 0; s < C::RF; ++s) {
+                const int row = kUp ? (s % (C::RF / 2)) * 16 + (s / (C::RF / 2)) * C::kUpFeat : s * 16;
+                f.a[s] = *reinterpret_cast<const i32x4_t*>(base + ((fbase + row * 128) ^ kx));
+            }
+        }
+    };
+    auto mma = [&](const Frags<C, N1>& f) {
+        if constexpr (NL > 0) {
+            __builtin_amdgcn_s_setprio(1);  // favour the wave that is issuing MFMAs
+#pragma unroll
+            for (int t = 0; t < NL; ++t)
+#pragma unroll
+                for (int s = 0; s < C::RF; ++s)
+                    acc[s][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(f.a[s], f.b[t], acc[s][t], 0, 0, 0);
+            __builtin_amdgcn_s_setprio(0);
+        }
+    };
+    wait_and_barrier<kLoads + C::kWLoads + C::kXLoads>();  // stage 0 of the S in flight has landed
+    Frags<C, N1> f0, f1;
+    read(0, 0u, f0);
+    int buf = 0;
+    for (int kt = 0; kt < nk; ++kt) {
+        read(buf, 64u, f1);
+        __builtin_amdgcn_sched_barrier(0);
+        mma(f0);
+        __builtin_amdgcn_sched_barrier(0);
+        // stage kt + 1 has landed and every wave has read all of stage kt
+        wait_and_barrier<kLoads>();
+        load(buf, kt + C::S);
+        buf = buf + 1 == C::S ? 0 : buf + 1;
+        read(buf, 0u, f0);  // past the last stage: zeros, unused
+        __builtin_amdgcn_sched_barrier(0);
+        mma(f1);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    __builtin_amdgcn_s_waitcnt(0x70);  // no load to LDS outlives the block
+}
+
+// Token of slot s (token 0 and a flag for a slot out of range).
+__device__ __forceinline__ int slot_token(const FfnI8Args& a, int s) {
+    if (s < 0 || s >= a.T * a.K) {
+        atomicOr(&a.ctrl[kWordFlags], (uint32_t)SPICE_FLAG_BAD_INDEX);
+        return 0;
+    }
+    return s / a.K;
+}
+
+template <bool kUp, class C>
+__global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2))) void i8_gemm_kernel(Job job) {
+    extern __shared__ __align__(16) unsigned char s_lds[];
+    const FfnI8Args& a = job.a;
+    Tile j;
+    if (!resolve<kUp, C>(job, xcd_tile(blockIdx.x, gridDim.x, C::kXcdBlocks), j)) return;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wf = w % C::WF, wt = w / C::WF;  // wave's feature part and token lane group
+    const int m = lane & 15, quad = lane >> 4;
+    const int frow0 = wf * ((kUp ? C::kUpFeat : C::BM) / C::WF);
+    // token sub-tiles of this wave with a live row
+    const int nlive = min(C::RT, max(0, (j.ntok - j.tok0 - 16 * wt + C::kTStride - 1) / C::kTStride));
+    i32x4_t acc[C::RF][C::RT];
+#pragma unroll
+    for (int s = 0; s < C::RF; ++s)
+#pragma unroll
+        for (int t = 0; t < C::RT; ++t) acc[s][t] = i32x4_t{0, 0, 0, 0};
+
+    // Staging: a loader wave's load writes 64 x 16 bytes to consecutive LDS, 8 staged rows of 8 chunks.
+    // Lane l fills LDS chunk l % 8 of row r0 = tid / 8 (+ kRowStep i), which holds the row's chunk
+    // (l % 8) ^ swizzle(row), so that is the chunk it fetches.
+    const int r0 = tid / 8;
+    const bool loader = C::kLoaders == C::kThreads || tid < C::kLoaders;
+    const int c16 = (int)((lds_off(r0, tid & 7) & 127u) >> 4);
+    const uint32_t ldx = kUp ? (uint32_t)a.d : (uint32_t)i8_row(j.kdim);
+    const uint32_t xrows = (uint32_t)(kUp || j.shared ? a.T : a.T * a.K);
+    const rsrc_t wbuf = raw_buffer(j.w, j.w_bytes);
+    const rsrc_t xbuf = raw_buffer(kUp ? a.xq : j.shared ? a.hqs : a.hq, xrows * ldx);
+    const uint32_t wstep = (uint32_t)j.kdim;
+    const uint32_t woff0 = (uint32_t)(j.row0 + r0) * wstep + c16 * 16;
+    const int klim = j.kdim - c16 * 16;  // the lane's chunk of stage kt is in the row while 128 kt < klim
+    const int nk = (j.kdim + kBK - 1) / kBK;
+    // Weight rows whose stride is a multiple of 2 KiB start on a few memory channels only: each weight
+    // tile starts its k order at another stage.
+    const int rot = wstep % 2048 == 0 ? (int)((uint32_t)(j.row0 / C::kUpFeat) * 5u % (uint32_t)nk) : 0;
+    // stage kt of the tile's nk; past the last one, a stage past the row
+    auto stage_k = [&](int kt) { return kt >= nk ? 0x800000 : kt + rot >= nk ? kt + rot - nk : kt + rot; };
+    auto load_w = [&](int buf, int kt) {
+        if (!loader) return;
+        unsigned char* run = s_lds + buf * C::kStage + w * 1024;
+        kt = stage_k(kt);
+        const bool in = kt * kBK < klim;
+#pragma unroll
+        for (int i = 0; i < C::kWLoads; ++i) {
+            const int r = C::kRowStep * i;
+            const uint32_t delta = (uint32_t)(kUp && r >= C::kUpFeat ? j.nfeat + r - C::kUpFeat : r) * wstep;
+            load_lds16(wbuf, in ? woff0 + delta + (uint32_t)kt * kBK : kOutOfRange, run + i * C::kRowStep * 128);
+        }
+    };
+    uint32_t xoff[C::kXLoads];
+    auto load_x = [&](int buf, int kt) {
+        if (!loader) return;
+        unsigned char* run = s_lds + buf * C::kStage + w * 1024 + C::kWTile;
+        kt = stage_k(kt);
+        const bool in = kt * kBK < klim;
+#pragma unroll
+        for (int i = 0; i < C::kXLoads; ++i)
+            load_lds16(xbuf, in && xoff[i] != kOutOfRange ? xoff[i] + (uint32_t)kt * kBK : kOutOfRange,
+                       run + i * C::kRowStep * 128);
+    };
+    auto load = [&](int buf, int kt) {
+        load_w(buf, kt);
+        load_x(buf, kt);
+    };
+    // the slot ids of the tile's rows, the weights of stage 0, then (once the ids are there) its token
+    // rows and the other stages of the ring
+    int sid[C::kXLoads];
+#pragma unroll
+    for (int i = 0; i < C::kXLoads; ++i) {
+        const int pos = j.tok0 + r0 + C::kRowStep * i;
+        sid[i] = -1;
+        if (loader && pos < j.ntok) sid[i] = (!kUp || j.shared) ? j.start + pos : a.perm[j.start + pos];
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    load_w(0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < C::kXLoads; ++i) {
+        const int pos = j.tok0 + r0 + C::kRowStep * i;
+        xoff[i] = kOutOfRange;
+        if (loader && pos < j.ntok) xoff[i] = (uint32_t)(!kUp || j.shared ? sid[i] : slot_token(a, sid[i])) * ldx + c16 * 16;
+    }
+    load_x(0, 0);
+#pragma unroll
+    for (int s = 1; s < C::S; ++s) load(s, s);
+
+    // LDS addresses of the fragments of k-step 0 (k-step 1 reads chunk c ^ 4: bit 6 flipped).  The swizzle
+    // of row r depends on (r >> 1) & 7, which steps of 16 rows leave unchanged.
+    const uint32_t fbase = lds_off(frow0 + m, quad);
+    const uint32_t tbase = C::kWTile + lds_off(wt * 16 + m, quad);
+    static_assert(C::RT == 2 || C::RT == 4, "token sub-tiles per wave");
+    if (nlive == C::RT) product<C, kUp, C::RT>(s_lds, nk, fbase, tbase, load, acc);
+    else if (nlive == 0) product<C, kUp, 0>(s_lds, nk, fbase, tbase, load, acc);
+    else if (nlive == 1) product<C, kUp, 1>(s_lds, nk, fbase, tbase, load, acc);
+    else if constexpr (C::RT > 2) {
+        if (nlive == 2) product<C, kUp, 2>(s_lds, nk, fbase, tbase, load, acc);
+        else product<C, kUp, 3>(s_lds, nk, fbase, tbase, load, acc);
+    }
+
+    // Epilogue: lane holds features 4 quad .. + 3 of sub-tile s for token m of sub-tile t.
+    const float* scale = reinterpret_cast<const float*>(j.w + j.w_bytes);
+#pragma unroll
+    for (int t = 0; t < C::RT; ++t) {
+        const int p = j.tok0 + t * C::kTStride + wt * 16 + m;
+        if (p >= j.ntok) continue;
+        const size_t pos = (size_t)j.start + p;
+        if constexpr (kUp) {
+            const float sx = a.xs[j.shared ? p : slot_token(a, a.perm[pos])];
+            float* dst = (j.shared ? a.hs : a.h) + pos * j.nfeat;
+#pragma unroll
+            for (int s = 0; s < C::RF / 2; ++s) {
+                const int f = j.row0 + frow0 + s * 16 + quad * 4;
+                if (f >= j.nfeat) continue;
+                const f32x4_t sg = *reinterpret_cast<const f32x4_t*>(scale + f);
+                const f32x4_t su = *reinterpret_cast<const f32x4_t*>(scale + j.nfeat + f);
+                f32x4_t h;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    h[i] = silu((float)acc[s][t][i] * (sx * sg[i])) * ((float)acc[s + C::RF / 2][t][i] * (sx * su[i]));
+                *reinterpret_cast<f32x4_t*>(dst + f) = h;
+            }
+        } else {
+            float sh = (j.shared ? a.hscale_s : a.hscale)[pos];
+            if (j.shared && a.sgate) sh *= a.sgate[pos];
+            float* dst = (j.shared ? a.y_shared : a.y_slots) + pos * a.d;
+#pragma unroll
+            for (int s = 0; s < C::RF; ++s) {
+                const int f = j.row0 + frow0 + s * 16 + quad * 4;
+                if (f >= a.d) continue;
+                const f32x4_t sc = *reinterpret_cast<const f32x4_t*>(scale + f);
+                f32x4_t y;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[i] = (float)acc[s][t][i] * (sh * sc[i]);
+                *reinterpret_cast<f32x4_t*>(dst + f) = y;
+            }
+        }
+    }
+}
+
+// Super-tile of the shared block: sn weight tiles x sm token tiles with sn | nt and sm | mt, at most one
+// XCD's resident blocks, as square as possible.
+void super_shape(int mt, int nt, int most, int32_t* out) {
+    int best_n = 1, best_m = 1, best_score = -1;
+    for (int sm = 1; sm <= mt && sm <= most; ++sm) {
+        if (mt % sm) continue;
+        for (int sn = 1; sn <= nt && sn * sm <= most; ++sn) {
+            if (nt % sn) continue;
+            const int score = sn * sm * 64 - (sn + sm);
+            if (score > best_score) { best_score = score; best_n = sn; best_m = sm; }
+        }
+    }
+    out[0] = best_n;
+    out[1] = best_m;
+}
+
+long long tiles_of(long long n, int per) { return (n + per - 1) / per; }
+
+template <bool kUp, class C>
+hipError_t launch_pass(const FfnI8Args& a, hipStream_t s) {
+    constexpr int feat = kUp ? C::kUpFeat : C::BM;
+    const long long slots = (long long)a.T * a.K, buckets = std::min<long long>(std::min(a.N, a.C), slots);
+    const long long nt_sh = tiles_of(kUp ? a.Is : a.d, feat), nt_e = tiles_of(kUp ? a.I : a.d, feat);
+    // upper bound: sum_e ceil(n_e / BT) <= slots / BT + buckets; blocks past the live tiles exit
+    const long long tiles = (a.Is > 0 ? tiles_of(a.T, C::BT) * nt_sh : 0) + (buckets > 0 ? (slots / C::BT + buckets) * nt_e : 0);
+    if (tiles == 0) return hipSuccess;
+    if (tiles > 0x7FFFFFFFll) return hipErrorInvalidValue;
+    Job job{a, {1, 1}};
+    if (a.Is > 0) super_shape((int)tiles_of(a.T, C::BT), (int)nt_sh, C::kXcdBlocks, job.super);
+    hipLaunchKernelGGL((i8_gemm_kernel<kUp, C>), dim3((unsigned)tiles), dim3(C::kThreads), C::S * C::kStage, s, job);
+    return hipGetLastError();
+}
+
+template <bool kUp>
+hipError_t launch_shape(const FfnI8Args& a, int shape, hipStream_t s) {
+    return shape == kGemmBig ? launch_pass<kUp, Big>(a, s) : shape == kGemmWide ? launch_pass<kUp, Wide>(a, s)
+                                                                                : launch_pass<kUp, Small>(a, s);
+}
+
+}  // namespace
+
+bool expert_gemm_i8_applies(const FfnI8Args& a) {
+    if (a.T < kI8GemmMinTokens) return false;
+    // offsets inside one operand are 32-bit
+    auto fits = [](long long rows, long long bytes) { return rows * bytes <= kMaxBuffer; };
+    const long long slots = (long long)a.T * a.K;
+    if (!fits(a.T, a.d) || !fits(slots, i8_row(a.I)) || !fits(a.T, i8_row(a.Is)) || !fits(2ll * a.I, a.d) ||
+        !fits(2ll * a.Is, a.d))
+        return false;
+    // the staged tiles need more LDS than the 64 KiB every AMD GPU offers
+    int dev = 0, lds = 0;
+    if (hipGetDevice(&dev) != hipSuccess) return false;
+    static int per_block[64] = {0};
+    if (dev < 0 || dev >= 64) return false;
+    if (per_block[dev] == 0) {
+        if (hipDeviceGetAttribute(&lds, hipDeviceAttributeMaxSharedMemoryPerBlock, dev) != hipSuccess) return false;
+        per_block[dev] = lds;
+    }
+    return per_block[dev] >= std::max({Big::S * Big::kStage, Wide::S * Wide::kStage, Small::S * Small::kStage});
+}
+
+hipError_t launch_expert_gemm_i8(const FfnI8Args& a, bool up, hipStream_t s) {
+    const int shape = gemm_shape(a.T, a.N, a.K, a.C, a.I, a.Is, SPICE_WFMT_DTYPE);
+    return up ? launch_shape<true>(a, shape, s) : launch_shape<false>(a, shape, s);
+}
+
+}  // namespace spice

@@ -368,6 +368,10 @@ hipError_t launch_shared_gate(const void* x, const void* w_sg, int32_t T, int32_
 hipError_t launch_expert_ffn_fetched(const FfnArgs& a, const FetchArgs& f, hipStream_t s);
 hipError_t launch_combine(const CombineArgs& a, hipStream_t s);
 hipError_t launch_expert_ffn_i8(const FfnI8Args& a, hipStream_t s);
+// Its up or down products as GEMM tiles (expert_gemm_i8.hip), for many tokens.
+constexpr int kI8GemmMinTokens = 64;
+bool expert_gemm_i8_applies(const FfnI8Args& a);
+hipError_t launch_expert_gemm_i8(const FfnI8Args& a, bool up, hipStream_t s);
 hipError_t launch_rmsnorm_quant(const NormArgs& a, hipStream_t s);
 hipError_t launch_spec_update(const SpecArgs& a, hipStream_t s);
 
