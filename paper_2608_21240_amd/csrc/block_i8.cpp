@@ -125,6 +125,8 @@ extern "C" spice_status_t moe_expert_ffn_grouped_i8(const spice_moe_cfg_t* cfg, 
         a.h = reinterpret_cast<float*>(wsb + L.h); a.hs = reinterpret_cast<float*>(wsb + L.hs);
         a.hq = reinterpret_cast<int8_t*>(wsb + L.hq); a.hqs = reinterpret_cast<int8_t*>(wsb + L.hqs);
         a.hscale = reinterpret_cast<float*>(wsb + L.hscale); a.hscale_s = reinterpret_cast<float*>(wsb + L.hscale_s);
+        a.top = reinterpret_cast<float*>(wsb + L.top); a.top_s = reinterpret_cast<float*>(wsb + L.top_s);
+        a.part = L.total > L.part && ws_bytes >= L.total ? reinterpret_cast<int32_t*>(wsb + L.part) : nullptr;
         a.ctrl = static_cast<uint32_t*>(ws);
         if (gated) {
             float* sg = reinterpret_cast<float*>(wsb + L.sgate);

@@ -5,39 +5,108 @@
 //   quant : per row of H, sh = max |h| / 127 and qh = round(h / sh)                          (int8)
 //   down  : Y[pos][j] = sh s2[j] sum_k W2[j][k] qh[k]                                         (fp32)
 //
-// The sums are int32 MFMAs (v_mfma_i32_16x16x64_i8) and exact, whatever their order; H stays fp32
-// until its row's maximum is known, so its only rounding to 8 bits is the one the format has.
+// The sums are int32 MFMAs (v_mfma_i32_16x16x64_i8) and exact, whatever their order; H stays fp32 until
+// its row's maximum is known, so its only rounding to 8 bits is the one the format has (bf16 in between
+// would move about 1 % of the codes).
+//
+// A block computes BM weight rows x BT tokens over the contraction, 128 k per stage, weights as the A
+// operand, tokens as B.  For `up` the rows are BM / 2 W1 rows and the same W3 rows, so a wave holds the
+// gate and up sums of its features and applies the scales and SwiGLU in registers.  A wave's token
+// sub-tiles are interleaved with the other waves' (rows kTStride t + 16 wt), so the ragged last tile of an
+// expert spreads over the SIMDs; sub-tiles without a live token are not read and issue no MFMA, and their
+// rows are not fetched.
+// Staging: buffer loads straight to LDS into a ring of S stages of 128-byte rows whose 16-byte chunks are
+// XOR-swizzled by row (chunk c of row r at c ^ ((r >> 1) & 7)).  A chunk past the end of a row, and a row
+// past the end of a matrix or a bucket, reads zero (an offset past the buffer).
+// Pipeline: the fragments of a stage's two k-steps are read half a stage ahead of their MFMAs; one barrier
+// per stage, in the middle of the MFMAs, frees the buffer just read for the stage S ahead.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <cmath>
 
+#include "route_last.h"
 #include "spice_internal.h"
 
 namespace spice {
 namespace {
 
+template <int BM_, int BT_, int WF_, int WT_, int S_, int L_>
+struct Shape {
+    static constexpr int BM = BM_, BT = BT_, WF = WF_, WT = WT_, S = S_;
+    static constexpr int kThreads = 64 * WF * WT;
+    static constexpr int kLoaders = 64 * L_;       // threads that issue the stages' loads
+    static constexpr int RF = BM / WF / 16;        // 16-row sub-tiles per wave
+    static constexpr int RT = BT / WT / 16;        // 16-token sub-tiles per wave
+    static constexpr int kTStride = 16 * WT;       // tile rows between a wave's token sub-tiles
+    static constexpr int kUpFeat = BM / 2;         // features of an up tile (W1 rows = W3 rows)
+    static constexpr int kTopGroup = kUpFeat / WF; // features of a wave: those of a partial maximum of H
+    static constexpr int kWTile = BM * 128;        // bytes of a stage's weight rows
+    static constexpr int kStage = (BM + BT) * 128;
+    static constexpr int kRowStep = kLoaders / 8;  // rows one load instruction of the loaders covers
+    static constexpr int kWLoads = BM / kRowStep, kXLoads = BT / kRowStep;
+    static constexpr int kXcdBlocks = 32 * std::max(1, 163840 / (S * kStage));  // resident blocks per XCD
+    static constexpr int kAccs = RF * RT * 4;      // sums per thread
+    static_assert(kRowStep % 16 == 0 && kUpFeat % kRowStep == 0, "staged rows keep their swizzle");
+    static_assert(BM % kRowStep == 0 && BT % kRowStep == 0, "whole load instructions");
+    static_assert((S - 1) * (kWLoads + kXLoads) < 64, "vmcnt holds the loads in flight");
+};
+using Tile64x32 = Shape<64, 32, 2, 2, 4, 4>;
+using Tile64x64 = Shape<64, 64, 2, 2, 3, 4>;
+using Tile128x64 = Shape<128, 64, 2, 2, 3, 4>;
+using Tile128x128 = Shape<128, 128, 2, 4, 2, 4>;
+using Tile256x256 = Shape<256, 256, 2, 4, 2, 4>;
+template <class C>
+constexpr bool matches(const I8Shape& s) {
+    return C::BM == s.rows && C::BT == s.tokens && C::S * C::kStage == s.lds;
+}
+static_assert(matches<Tile64x32>(kI8Shapes[0]) && matches<Tile64x64>(kI8Shapes[1]) && matches<Tile128x64>(kI8Shapes[2]) &&
+                  matches<Tile128x128>(kI8Shapes[3]) && matches<Tile256x256>(kI8Shapes[4]),
+              "the shapes as the rules know them");
+
+constexpr int kBK = 128;                         // contraction per stage
+constexpr uint32_t kOutOfRange = 0xFFFFFFF0u;    // an offset past every buffer
+constexpr int kRawBufferWord3 = 0x00020000;      // gfx9 raw buffer: 32-bit data format
+
 typedef int i32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
-constexpr int kThreads = 256, kWaves = 4;
-constexpr int kTok = 16;  // tokens of a tile
-
 __device__ __forceinline__ float silu(float u) { return u / (1.0f + __expf(-u)); }
 
-// A tile of a launch: which matrix, which rows of it and which tokens.
-struct Tile {
-    bool shared;
-    const char* w;       // the matrix's blob: codes, then the scales of its rows
-    int row0;            // first feature
-    int tok0, ntok;      // first token of the tile in its group, tokens of the group
-    int start;           // the group's first bucket position (0 for the shared block)
+__device__ __forceinline__ float max_or_nan(float a, float b) {
+    return a != a || b != b ? __builtin_nanf("") : fmaxf(a, b);
+}
+
+// Logical tile of block b: rounds of 8 x per_xcd blocks give each XCD (block b runs on XCD b % 8) per_xcd
+// consecutive tiles, which share operands in that XCD's L2.  A bijection on [0, G).
+__device__ __forceinline__ int xcd_tile(int b, int G, int per_xcd) {
+    const int round = 8 * per_xcd;
+    if (b >= (G / round) * round) return b;
+    const int x = b & 7, slot = b >> 3;
+    return (slot / per_xcd) * round + x * per_xcd + slot % per_xcd;
+}
+
+struct Job {
+    FfnI8Args a;
+    int32_t super[2];  // shared-block super-tile (weight tiles, token tiles)
+    int32_t parts;     // splits of the shared block's down contraction
+    int32_t xcd;       // whether neighbouring tiles run on one XCD
 };
 
-// The HIT bucket that holds tile L, of nt weight tiles per token tile, found by a wave's scan of the
-// offsets (uniform results); false past the last one.
-__device__ bool find_bucket(const FfnI8Args& a, int nt, int& L, int& e_, int& st_, int& n_) {
-    const int lane = threadIdx.x & 63;
+struct Tile {
+    bool shared;
+    const char* w;        // the matrix's blob
+    uint32_t w_bytes;     // of its codes
+    int kdim, nfeat;      // contraction, output features
+    int row0;             // first feature
+    int tok0, ntok;       // first token of the tile in its group, tokens of the group
+    int start;            // the group's first bucket position (0 for the shared block)
+    int k0, k1;           // stages of the contraction this tile takes
+    int split;            // which of the shared block's output tiles, where its contraction is split; or -1
+    int part;             // and which part of it
+};
+
+// The HIT bucket holding tile L of nt tiles per token tile, by a wave's scan of the offsets.
+__device__ bool find_bucket(const FfnI8Args& a, int nt, int BT, int& L, int lane, int& e_, int& st_, int& n_) {
     const int32_t* off = a.offsets + SPICE_CLASS_HIT * (a.N + 1);
     for (int e0 = 0; e0 < a.N; e0 += 64) {
         const int e = e0 + lane;
@@ -47,7 +116,7 @@ __device__ bool find_bucket(const FfnI8Args& a, int nt, int& L, int& e_, int& st
             n = off[e + 1] - st;
         }
         if (n > a.T * a.K) n = 0;
-        const int tiles = n > 0 ? ((n + kTok - 1) / kTok) * nt : 0;
+        const int tiles = n > 0 ? ((n + BT - 1) / BT) * nt : 0;
         int incl = tiles;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
@@ -69,212 +138,462 @@ __device__ bool find_bucket(const FfnI8Args& a, int nt, int& L, int& e_, int& st
     return false;
 }
 
-template <bool kUp, int kFeat>
-__device__ bool find_tile(const FfnI8Args& a, int L, Tile& t) {
-    const int mt_sh = (a.T + kTok - 1) / kTok;
-    const int nt_sh = ((kUp ? a.Is : a.d) + kFeat - 1) / kFeat, nt_e = ((kUp ? a.I : a.d) + kFeat - 1) / kFeat;
-    const int tiles_sh = a.Is > 0 ? nt_sh * mt_sh : 0;
+// Logical tile L of a launch (every wave resolves it for itself): the shared block's tiles first, in
+// groups of about an XCD's blocks that share operand tiles in its L2, then the HIT buckets in id order,
+// the token tiles of one weight tile next to each other.
+template <bool kUp, class C>
+__device__ bool resolve(const Job& job, int L, Tile& j) {
+    const FfnI8Args& a = job.a;
+    constexpr int feat = kUp ? C::kUpFeat : C::BM;
+    const int nt_sh = ((kUp ? a.Is : a.d) + feat - 1) / feat, nt_e = ((kUp ? a.I : a.d) + feat - 1) / feat;
+    const int mt_sh = (a.T + C::BT - 1) / C::BT;
+    const int parts = kUp ? 1 : job.parts, per_part = nt_sh * mt_sh;
+    const int tiles_sh = a.Is > 0 ? per_part * parts : 0;
+    j.k0 = 0;
+    j.split = -1;
+    j.part = 0;
     if (L < tiles_sh) {
-        t.shared = true;
-        t.w = kUp ? a.w13s : a.w2s;
-        t.row0 = L / mt_sh * kFeat;
-        t.tok0 = L % mt_sh * kTok;
-        t.ntok = a.T;
-        t.start = 0;
+        j.part = L / per_part;
+        L -= j.part * per_part;
+        if (parts > 1) j.split = L;
+        const int sn = job.super[0], sm = job.super[1];
+        const int g = L / (sn * sm), in = L - g * (sn * sm), mg = mt_sh / sm;
+        j.shared = true;
+        j.w = kUp ? a.w13s : a.w2s;
+        j.w_bytes = (uint32_t)(kUp ? 2 : 1) * (uint32_t)a.Is * (uint32_t)a.d;
+        j.kdim = kUp ? a.d : a.Is;
+        j.nfeat = kUp ? a.Is : a.d;
+        j.row0 = ((g / mg) * sn + in / sm) * feat;
+        j.tok0 = ((g % mg) * sm + in % sm) * C::BT;
+        j.ntok = a.T;
+        j.start = 0;
+        const int nk = (j.kdim + kBK - 1) / kBK;
+        j.k0 = j.part * nk / parts;
+        j.k1 = (j.part + 1) * nk / parts;
         return true;
     }
     L -= tiles_sh;
-    int e, st, n;
-    if (a.C <= 0 || !find_bucket(a, nt_e, L, e, st, n)) return false;
+    int e = 0, st = 0, n = 0;
+    if (a.C <= 0 || !find_bucket(a, nt_e, C::BT, L, threadIdx.x & 63, e, st, n)) return false;
     const int slot = a.resident_slot[e];
     if (st < 0 || st + n > a.T * a.K || slot < 0 || slot >= a.C) {
         if (threadIdx.x == 0)
             atomicOr(&a.ctrl[kWordFlags], (uint32_t)(slot < 0 || slot >= a.C ? SPICE_FLAG_BAD_SLOT : SPICE_FLAG_BAD_INDEX));
         return false;
     }
-    const int mt = (n + kTok - 1) / kTok;
+    const int mt = (n + C::BT - 1) / C::BT, nn = L / mt;
     const size_t elems = (size_t)(kUp ? 2 : 1) * a.I * a.d, rows = kUp ? 2 * (size_t)a.I : (size_t)a.d;
-    t.shared = false;
-    t.w = (kUp ? a.w13_pool : a.w2_pool) + (size_t)slot * (elems + 4 * rows);
-    t.row0 = L / mt * kFeat;
-    t.tok0 = L % mt * kTok;
-    t.ntok = n;
-    t.start = st;
+    j.shared = false;
+    j.w = (kUp ? a.w13_pool : a.w2_pool) + (size_t)slot * (elems + 4 * rows);
+    j.w_bytes = (uint32_t)elems;
+    j.kdim = kUp ? a.d : a.I;
+    j.nfeat = kUp ? a.I : a.d;
+    j.row0 = nn * feat;
+    j.tok0 = (L - nn * mt) * C::BT;
+    j.ntok = n;
+    j.start = st;
+    j.k1 = (j.kdim + kBK - 1) / kBK;
     return true;
 }
 
-constexpr int kDepth = 4;  // 64-byte steps in flight per wave and row stream
-
-// Sums of NR row streams (16 rows each, 16 bytes per lane and step) with 16 tokens, over the wave's
-// share of the contraction; lane (m, quad) holds bytes 16 quad .. 16 quad + 15 of a step of row m and
-// token m.  Bytes past the row are read as the row's first ones, with the token's taken as 0.
-template <int NR>
-__device__ __forceinline__ void wave_sums(const char* const (&wr)[NR], const char* xr, bool live, int K, i32x4_t (&acc)[NR]) {
-    const int lane = threadIdx.x & 63, quad = lane >> 4;
-    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int nst = (K + 63) / 64, s0 = w * nst / kWaves, s1 = (w + 1) * nst / kWaves;
-    for (int s = s0; s < s1; s += kDepth) {
-        i32x4_t wv[kDepth][NR], xv[kDepth];
-#pragma unroll
-        for (int u = 0; u < kDepth; ++u) {
-            const int k = (s + u) * 64 + quad * 16;
-            const bool in = s + u < s1 && k < K;
-            const int at = in ? k : 0;
-#pragma unroll
-            for (int r = 0; r < NR; ++r) wv[u][r] = *reinterpret_cast<const i32x4_t*>(wr[r] + at);
-            xv[u] = i32x4_t{0, 0, 0, 0};
-            if (in && live) xv[u] = *reinterpret_cast<const i32x4_t*>(xr + k);
-        }
-#pragma unroll
-        for (int u = 0; u < kDepth; ++u)
-#pragma unroll
-            for (int r = 0; r < NR; ++r) acc[r] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[u][r], xv[u], acc[r], 0, 0, 0);
-    }
+// Byte offset of 16-byte chunk c of staged row r inside an operand tile.
+__device__ __forceinline__ uint32_t lds_off(int r, int c) {
+    return (uint32_t)(r * 128 + ((c ^ ((r >> 1) & 7)) << 4));
 }
 
-// Up: 16 features (16 gate and 16 up rows) x 16 tokens per block, the contraction split over the waves.
-__global__ __launch_bounds__(kThreads) void i8_up_kernel(FfnI8Args a) {
-    __shared__ int s_red[2][kWaves][16][17];  // [gate / up][wave][token][feature]
-    Tile t;
-    if (!find_tile<true, 16>(a, blockIdx.x, t)) return;
-    const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, quad = lane >> 4, w = tid >> 6;
-    const int nf = t.shared ? a.Is : a.I, d = a.d;
-    auto token = [&](int p) -> int {  // the token of the tile's p-th column, or -1
-        if (t.tok0 + p >= t.ntok) return -1;
-        if (t.shared) return t.tok0 + p;
-        const int s = a.perm[t.start + t.tok0 + p];
-        if (s >= 0 && s < a.T * a.K) return s / a.K;
+typedef __amdgpu_buffer_rsrc_t rsrc_t;
+__device__ __forceinline__ rsrc_t raw_buffer(const void* p, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)bytes, kRawBufferWord3);
+}
+
+// 16 bytes from offset off of a buffer to LDS byte lds + 16 * lane, lds uniform over the wave (counted by
+// vmcnt; an offset past the buffer writes zeros).  Device pass only: the host pass of a kernel naming
+// this target builtin would lose its launch stub.
+__device__ __forceinline__ void load_lds16(rsrc_t b, uint32_t off, unsigned char* lds) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (__attribute__((address_space(3))) void*)lds, 16, (int)off, 0, 0, 0);
+#endif
+}
+
+// s_waitcnt with vmcnt(n) lgkmcnt(0), then the block's barrier: no wait for loads to LDS beyond those
+// the caller names (a __syncthreads would drain them all).
+template <int n>
+__device__ __forceinline__ void wait_and_barrier() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((n & 15) | ((n >> 4) << 14) | 0x70);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Fragments of one 64-k step: RF weight sub-tiles and the NL live token sub-tiles.
+template <class C, int NL>
+struct Frags {
+    i32x4_t a[C::RF], b[NL];
+};
+
+// The main loop of one tile with NL live token sub-tiles in this wave (NL = 0: the wave only loads and
+// keeps the barriers).
+template <class C, bool kUp, int NL, class Load>
+__device__ __forceinline__ void product(unsigned char* s_lds, int nk, uint32_t fbase, uint32_t tbase, Load load,
+                                        i32x4_t (&acc)[C::RF][C::RT]) {
+    constexpr int N1 = NL > 0 ? NL : 1;
+    constexpr int kLoads = (C::S - 2) * (C::kWLoads + C::kXLoads);  // stages in flight past the next one
+    auto read = [&](int buf, uint32_t kx, Frags<C, N1>& f) {
+        if constexpr (NL > 0) {
+            const unsigned char* base = s_lds + buf * C::kStage;
+#pragma unroll
+            for (int t = 0; t < NL; ++t)
+                f.b[t] = *reinterpret_cast<const i32x4_t*>(base + ((tbase + t * C::kTStride * 128) ^ kx));
+#pragma unroll
+            for (int s = 0; s < C::RF; ++s) {
+                const int row = kUp ? (s % (C::RF / 2)) * 16 + (s / (C::RF / 2)) * C::kUpFeat : s * 16;
+                f.a[s] = *reinterpret_cast<const i32x4_t*>(base + ((fbase + row * 128) ^ kx));
+            }
+        }
+    };
+    auto mma = [&](const Frags<C, N1>& f) {
+        if constexpr (NL > 0) {
+            __builtin_amdgcn_s_setprio(1);  // favour the wave that is issuing MFMAs
+#pragma unroll
+            for (int t = 0; t < NL; ++t)
+#pragma unroll
+                for (int s = 0; s < C::RF; ++s)
+                    acc[s][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(f.a[s], f.b[t], acc[s][t], 0, 0, 0);
+            __builtin_amdgcn_s_setprio(0);
+        }
+    };
+    wait_and_barrier<kLoads + C::kWLoads + C::kXLoads>();  // stage 0 of the S in flight has landed
+    Frags<C, N1> f0, f1;
+    read(0, 0u, f0);
+    int buf = 0;
+    for (int kt = 0; kt < nk; ++kt) {
+        read(buf, 64u, f1);
+        __builtin_amdgcn_sched_barrier(0);
+        mma(f0);
+        __builtin_amdgcn_sched_barrier(0);
+        // stage kt + 1 has landed and every wave has read all of stage kt
+        wait_and_barrier<kLoads>();
+        load(buf, kt + C::S);
+        buf = buf + 1 == C::S ? 0 : buf + 1;
+        read(buf, 0u, f0);  // past the last stage: zeros, unused
+        __builtin_amdgcn_sched_barrier(0);
+        mma(f1);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    __builtin_amdgcn_s_waitcnt(0x70);  // no load to LDS outlives the block
+}
+
+// Token of slot s (token 0 and a flag for a slot out of range).
+__device__ __forceinline__ int slot_token(const FfnI8Args& a, int s) {
+    if (s < 0 || s >= a.T * a.K) {
         atomicOr(&a.ctrl[kWordFlags], (uint32_t)SPICE_FLAG_BAD_INDEX);
         return 0;
-    };
-    const int tok = token(m);
-    const char* rows[2] = {t.w + (size_t)(t.row0 + m) * d, t.w + (size_t)(nf + t.row0 + m) * d};
-    i32x4_t acc[2] = {};
-    wave_sums<2>(rows, reinterpret_cast<const char*>(a.xq) + (size_t)(tok < 0 ? 0 : tok) * d, tok >= 0, d, acc);
-#pragma unroll
-    for (int r = 0; r < 2; ++r)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s_red[r][w][m][quad * 4 + i] = acc[r][i];
-    __syncthreads();
-    const int p = tid >> 4, f = tid & 15;
-    const int tp = token(p);
-    if (tp < 0) return;
-    int g = 0, u = 0;
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
-        g += s_red[0][i][p][f];
-        u += s_red[1][i][p][f];
     }
-    const float* scale = reinterpret_cast<const float*>(t.w + (size_t)2 * nf * d);
-    const float sx = a.xs[tp];
-    const float gv = (float)g * (sx * scale[t.row0 + f]), uv = (float)u * (sx * scale[nf + t.row0 + f]);
-    float* h = t.shared ? a.hs : a.h;
-    h[(size_t)(t.start + t.tok0 + p) * nf + t.row0 + f] = silu(gv) * uv;
+    return s / a.K;
 }
 
-// Rows of H to 8 bits: a block per row; the T shared rows first, then the HIT slots' positions.
-__global__ __launch_bounds__(kThreads) void i8_quant_kernel(FfnI8Args a) {
-    __shared__ float s_top[kWaves];
-    const int nsh = a.Is > 0 ? a.T : 0;
-    const bool shared = (int)blockIdx.x < nsh;
-    const int row = shared ? blockIdx.x : blockIdx.x - nsh;
-    if (!shared && row >= a.offsets[a.N]) return;  // the HIT buckets' end
-    const int tid = threadIdx.x, n = shared ? a.Is : a.I;
-    const float* h = (shared ? a.hs : a.h) + (size_t)row * n;
-    int8_t* q = (shared ? a.hqs : a.hq) + (size_t)row * i8_row(n);
-    float top = 0.f, bad = 0.f;
-    for (int i = tid * 4; i < n; i += kThreads * 4) {
-        const f32x4_t v = *reinterpret_cast<const f32x4_t*>(h + i);
+// Leaves a part's sums at the device-coherent level and counts it; true for the last of the tile's parts,
+// whose acc then holds the sum of all.
+template <class C>
+__device__ __forceinline__ bool split_sums(const FfnI8Args& a, int parts, int tile, int mine, int32_t* part,
+                                           i32x4_t (&acc)[C::RF][C::RT], int* s_last) {
+    int32_t* own = part + (size_t)mine * C::kAccs * C::kThreads;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            top = fmaxf(top, fabsf(v[k]));
-            bad = fmaf(v[k], 0.f, bad);
+    for (int s = 0; s < C::RF; ++s)
+#pragma unroll
+        for (int t = 0; t < C::RT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                __hip_atomic_store(own + ((s * C::RT + t) * 4 + i) * C::kThreads, acc[s][t][i], __ATOMIC_RELAXED,
+                                   __HIP_MEMORY_SCOPE_AGENT);
+    if (!route_last_block(&a.ctrl[kWordI8Parts + tile], parts, s_last)) return false;
+    for (int p = 0; p < parts; ++p) {
+        if (p == mine) continue;
+        const int32_t* other = part + (size_t)p * C::kAccs * C::kThreads;
+#pragma unroll
+        for (int s = 0; s < C::RF; ++s)
+#pragma unroll
+            for (int t = 0; t < C::RT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    acc[s][t][i] += __hip_atomic_load(other + ((s * C::RT + t) * 4 + i) * C::kThreads, __ATOMIC_RELAXED,
+                                                      __HIP_MEMORY_SCOPE_AGENT);
+    }
+    return true;
+}
+
+template <bool kUp, class C>
+__global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2))) void i8_gemm_kernel(Job job) {
+    extern __shared__ __align__(16) unsigned char s_lds[];
+    const FfnI8Args& a = job.a;
+    Tile j;
+    __shared__ int s_last;
+    if (!resolve<kUp, C>(job, job.xcd ? xcd_tile(blockIdx.x, gridDim.x, C::kXcdBlocks) : (int)blockIdx.x, j)) return;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wf = w % C::WF, wt = w / C::WF;  // wave's feature part and token lane group
+    const int m = lane & 15, quad = lane >> 4;
+    const int frow0 = wf * ((kUp ? C::kUpFeat : C::BM) / C::WF);
+    // token sub-tiles of this wave with a live row
+    const int nlive = min(C::RT, max(0, (j.ntok - j.tok0 - 16 * wt + C::kTStride - 1) / C::kTStride));
+    i32x4_t acc[C::RF][C::RT];
+#pragma unroll
+    for (int s = 0; s < C::RF; ++s)
+#pragma unroll
+        for (int t = 0; t < C::RT; ++t) acc[s][t] = i32x4_t{0, 0, 0, 0};
+
+    // Staging: a loader wave's load writes 64 x 16 bytes to consecutive LDS, 8 staged rows of 8 chunks.
+    // Lane l fills LDS chunk l % 8 of row r0 = tid / 8 (+ kRowStep i), which holds the row's chunk
+    // (l % 8) ^ swizzle(row), so that is the chunk it fetches.
+    const int r0 = tid / 8;
+    const bool loader = C::kLoaders == C::kThreads || tid < C::kLoaders;
+    const int c16 = (int)((lds_off(r0, tid & 7) & 127u) >> 4);
+    const uint32_t ldx = kUp ? (uint32_t)a.d : (uint32_t)i8_row(j.kdim);
+    // up: all tokens' rows (512 MiB at most); down: the tile's, which are consecutive
+    const size_t row_first = (size_t)j.start + j.tok0;
+    const rsrc_t wbuf = raw_buffer(j.w, j.w_bytes);
+    const rsrc_t xbuf = kUp ? raw_buffer(a.xq, (uint32_t)a.T * ldx)
+                            : raw_buffer((j.shared ? a.hqs : a.hq) + row_first * ldx, (uint32_t)min(C::BT, j.ntok - j.tok0) * ldx);
+    const uint32_t wstep = (uint32_t)j.kdim;
+    const uint32_t woff0 = (uint32_t)(j.row0 + r0) * wstep + c16 * 16;
+    const int klim = j.kdim - c16 * 16;  // the lane's chunk of stage kt is in the row while 128 kt < klim
+    const int nk = j.k1 - j.k0;
+    // Weight rows whose stride is a multiple of 2 KiB start on a few memory channels only: each weight
+    // tile starts its k order at another stage.
+    const int rot = wstep % 2048 == 0 ? (int)((uint32_t)(j.row0 / C::kUpFeat) * 5u % (uint32_t)nk) : 0;
+    // stage kt of the tile's nk; past the last one, a stage past the row
+    auto stage_k = [&](int kt) { return kt >= nk ? 0x800000 : j.k0 + (kt + rot >= nk ? kt + rot - nk : kt + rot); };
+    auto load_w = [&](int buf, int kt) {
+        if (!loader) return;
+        unsigned char* run = s_lds + buf * C::kStage + w * 1024;
+        kt = stage_k(kt);
+        const bool in = kt * kBK < klim;
+#pragma unroll
+        for (int i = 0; i < C::kWLoads; ++i) {
+            const int r = C::kRowStep * i;
+            const uint32_t delta = (uint32_t)(kUp && r >= C::kUpFeat ? j.nfeat + r - C::kUpFeat : r) * wstep;
+            load_lds16(wbuf, in ? woff0 + delta + (uint32_t)kt * kBK : kOutOfRange, run + i * C::kRowStep * 128);
+        }
+    };
+    uint32_t xoff[C::kXLoads];
+    auto load_x = [&](int buf, int kt) {
+        if (!loader) return;
+        unsigned char* run = s_lds + buf * C::kStage + w * 1024 + C::kWTile;
+        kt = stage_k(kt);
+        const bool in = kt * kBK < klim;
+#pragma unroll
+        for (int i = 0; i < C::kXLoads; ++i)
+            load_lds16(xbuf, in && xoff[i] != kOutOfRange ? xoff[i] + (uint32_t)kt * kBK : kOutOfRange,
+                       run + i * C::kRowStep * 128);
+    };
+    auto load = [&](int buf, int kt) {
+        load_w(buf, kt);
+        load_x(buf, kt);
+    };
+    // the slot ids of the tile's rows, the weights of stage 0, then (once the ids are there) its token
+    // rows and the other stages of the ring
+    int sid[C::kXLoads];
+#pragma unroll
+    for (int i = 0; i < C::kXLoads; ++i) {
+        const int pos = j.tok0 + r0 + C::kRowStep * i;
+        sid[i] = -1;
+        if (loader && pos < j.ntok) sid[i] = !kUp ? pos - j.tok0 : j.shared ? pos : a.perm[j.start + pos];
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    load_w(0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < C::kXLoads; ++i) {
+        const int pos = j.tok0 + r0 + C::kRowStep * i;
+        xoff[i] = kOutOfRange;
+        if (loader && pos < j.ntok) xoff[i] = (uint32_t)(!kUp || j.shared ? sid[i] : slot_token(a, sid[i])) * ldx + c16 * 16;
+    }
+    load_x(0, 0);
+#pragma unroll
+    for (int s = 1; s < C::S; ++s) load(s, s);
+
+    // LDS addresses of the fragments of k-step 0 (k-step 1 reads chunk c ^ 4: bit 6 flipped).  The swizzle
+    // of row r depends on (r >> 1) & 7, which steps of 16 rows leave unchanged.
+    const uint32_t fbase = lds_off(frow0 + m, quad);
+    const uint32_t tbase = C::kWTile + lds_off(wt * 16 + m, quad);
+    static_assert(C::RT == 1 || C::RT == 2 || C::RT == 4, "token sub-tiles per wave");
+    if (nlive == C::RT) product<C, kUp, C::RT>(s_lds, nk, fbase, tbase, load, acc);
+    else if (nlive == 0) product<C, kUp, 0>(s_lds, nk, fbase, tbase, load, acc);
+    else if constexpr (C::RT > 2) {
+        if (nlive == 1) product<C, kUp, 1>(s_lds, nk, fbase, tbase, load, acc);
+        else if (nlive == 2) product<C, kUp, 2>(s_lds, nk, fbase, tbase, load, acc);
+        else product<C, kUp, 3>(s_lds, nk, fbase, tbase, load, acc);
+    } else if constexpr (C::RT > 1) {
+        product<C, kUp, 1>(s_lds, nk, fbase, tbase, load, acc);
+    }
+
+    if constexpr (!kUp) {
+        if (j.split >= 0) {
+            // the last of the tile's parts to arrive adds the others' sums to its own (exact: in any order)
+            int32_t* part = a.part + (size_t)j.split * job.parts * C::kAccs * C::kThreads + tid;
+            if (!split_sums<C>(a, job.parts, j.split, j.part, part, acc, &s_last)) return;
         }
     }
-    top += bad;  // NaN for a row that is not finite
+
+    // Epilogue: lane holds features 4 quad .. + 3 of sub-tile s for token m of sub-tile t.
+    const float* scale = reinterpret_cast<const float*>(j.w + j.w_bytes);
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        const float other = __shfl_xor(top, o);
-        top = other != other || top != top ? __builtin_nanf("") : fmaxf(top, other);
+    for (int t = 0; t < C::RT; ++t) {
+        const int p = j.tok0 + t * C::kTStride + wt * 16 + m;
+        if (p >= j.ntok) continue;
+        const size_t pos = (size_t)j.start + p;
+        if constexpr (kUp) {
+            const float sx = a.xs[j.shared ? p : slot_token(a, a.perm[pos])];
+            float* dst = (j.shared ? a.hs : a.h) + pos * j.nfeat;
+            float top = 0.f, bad = 0.f;  // bad: NaN once a value is not finite
+#pragma unroll
+            for (int s = 0; s < C::RF / 2; ++s) {
+                const int f = j.row0 + frow0 + s * 16 + quad * 4;
+                if (f >= j.nfeat) continue;
+                const f32x4_t sg = *reinterpret_cast<const f32x4_t*>(scale + f);
+                const f32x4_t su = *reinterpret_cast<const f32x4_t*>(scale + j.nfeat + f);
+                f32x4_t h;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    h[i] = silu((float)acc[s][t][i] * (sx * sg[i])) * ((float)acc[s + C::RF / 2][t][i] * (sx * su[i]));
+                *reinterpret_cast<f32x4_t*>(dst + f) = h;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    top = fmaxf(top, fabsf(h[i]));
+                    bad = fmaf(h[i], 0.f, bad);
+                }
+            }
+            // the row's partial maximum over the wave's features
+            top += bad;
+            top = max_or_nan(top, __shfl_xor(top, 16));
+            top = max_or_nan(top, __shfl_xor(top, 32));
+            const int f0 = j.row0 + frow0;
+            if (quad == 0 && f0 < j.nfeat) (j.shared ? a.top_s : a.top)[pos * (j.nfeat / 16) + f0 / C::kTopGroup] = top;
+        } else {
+            float sh = (j.shared ? a.hscale_s : a.hscale)[pos];
+            if (j.shared && a.sgate) sh *= a.sgate[pos];
+            float* dst = (j.shared ? a.y_shared : a.y_slots) + pos * a.d;
+#pragma unroll
+            for (int s = 0; s < C::RF; ++s) {
+                const int f = j.row0 + frow0 + s * 16 + quad * 4;
+                if (f >= a.d) continue;
+                const f32x4_t sc = *reinterpret_cast<const f32x4_t*>(scale + f);
+                f32x4_t y;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[i] = (float)acc[s][t][i] * (sh * sc[i]);
+                *reinterpret_cast<f32x4_t*>(dst + f) = y;
+            }
+        }
     }
+}
+
+// Rows of H to 8 bits: a block per kQuantRow values of a row, the T shared rows first, then the HIT slots'
+// positions.  The row's maximum comes from the partial maxima that the up tiles left, one per `group`
+// features, so a row's blocks need not wait for each other; the values are on their way meanwhile.
+constexpr int kQuantThreads = 256;
+constexpr int kQuantVec = 4;  // 16-byte chunks per thread
+constexpr int kQuantRow = kQuantVec * 4 * kQuantThreads;
+__global__ __launch_bounds__(kQuantThreads) void i8_quant_kernel(FfnI8Args a, int nsh, int segs_sh, int segs, int group) {
+    __shared__ float s_top[kQuantThreads / 64];
+    const bool shared = (int)blockIdx.x < nsh * segs_sh;
+    const int b = shared ? blockIdx.x : blockIdx.x - nsh * segs_sh, per = shared ? segs_sh : segs;
+    const int row = b / per, seg = b - row * per;
+    if (!shared && row >= a.offsets[a.N]) return;  // the HIT buckets' end
+    const int tid = threadIdx.x, n = shared ? a.Is : a.I, nv = n / 4, nt = (n + group - 1) / group;
+    const f32x4_t* h = reinterpret_cast<const f32x4_t*>((shared ? a.hs : a.h) + (size_t)row * n);
+    const float* part = (shared ? a.top_s : a.top) + (size_t)row * (n / 16);
+    uint32_t* q = reinterpret_cast<uint32_t*>((shared ? a.hqs : a.hq) + (size_t)row * i8_row(n));
+    const int i0 = seg * (kQuantRow / 4) + tid;
+    f32x4_t v[kQuantVec];
+#pragma unroll
+    for (int c = 0; c < kQuantVec; ++c)
+        if (c == 0 || seg * (kQuantRow / 4) + c * kQuantThreads < nv) v[c] = h[min(i0 + c * kQuantThreads, nv - 1)];
+    float top = 0.f;
+    for (int i = tid; i < nt; i += kQuantThreads) top = max_or_nan(top, part[i]);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = max_or_nan(top, __shfl_xor(top, o));
     if ((tid & 63) == 0) s_top[tid >> 6] = top;
     __syncthreads();
-    top = 0.f;
+    top = s_top[0];
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) top = s_top[i] != s_top[i] || top != top ? __builtin_nanf("") : fmaxf(top, s_top[i]);
-    const bool nan = top != top;
-    const float inv = nan || top == 0.f ? 0.f : 127.f / top;
-    if (tid == 0) (shared ? a.hscale_s : a.hscale)[row] = top / 127.f;
-    for (int i = tid * 4; i < n; i += kThreads * 4) {
-        const f32x4_t v = *reinterpret_cast<const f32x4_t*>(h + i);
-        uint32_t b = 0;
+    for (int i = 1; i < kQuantThreads / 64; ++i) top = max_or_nan(top, s_top[i]);
+    if (tid == 0 && seg == 0) (shared ? a.hscale_s : a.hscale)[row] = top / 127.f;
+    // a row that is not finite has a maximum of NaN: codes 0, and the scale NaN
+    const float inv = top > 0.f ? 127.f / top : 0.f;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) b |= (uint32_t)((int)(nan ? 0.f : rintf(v[k] * inv)) & 255) << (8 * k);
-        *reinterpret_cast<uint32_t*>(q + i) = b;
+    for (int c = 0; c < kQuantVec; ++c) {
+        const int i = i0 + c * kQuantThreads;
+        if (i >= nv) break;
+        uint32_t bits = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) bits |= (uint32_t)((int)rintf(inv == 0.f ? 0.f : v[c][k] * inv) & 255) << (8 * k);
+        q[i] = bits;
     }
 }
 
-// Down: 32 output features x 16 tokens per block, the contraction split over the waves.
-constexpr int kDownR = 2;
-__global__ __launch_bounds__(kThreads) void i8_down_kernel(FfnI8Args a) {
-    __shared__ int s_red[kDownR][kWaves][16][17];
-    Tile t;
-    if (!find_tile<false, 16 * kDownR>(a, blockIdx.x, t)) return;
-    const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, quad = lane >> 4, w = tid >> 6;
-    const int K = t.shared ? a.Is : a.I, d = a.d;
-    const char* rows[kDownR];
-#pragma unroll
-    for (int r = 0; r < kDownR; ++r) rows[r] = t.w + (size_t)min(t.row0 + 16 * r + m, d - 1) * K;
-    const bool live = t.tok0 + m < t.ntok;
-    const char* x = reinterpret_cast<const char*>(t.shared ? a.hqs : a.hq) +
-                    (size_t)(live ? t.start + t.tok0 + m : 0) * i8_row(K);
-    i32x4_t acc[kDownR] = {};
-    wave_sums<kDownR>(rows, x, live, K, acc);
-#pragma unroll
-    for (int r = 0; r < kDownR; ++r)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s_red[r][w][m][quad * 4 + i] = acc[r][i];
-    __syncthreads();
-    const int p = tid >> 4, f = tid & 15;
-    if (t.tok0 + p >= t.ntok) return;
-    const int pos = t.start + t.tok0 + p;
-    const float* scale = reinterpret_cast<const float*>(t.w + (size_t)d * K);
-    float sh = (t.shared ? a.hscale_s : a.hscale)[pos];
-    if (t.shared && a.sgate) sh *= a.sgate[pos];
-    float* y = (t.shared ? a.y_shared : a.y_slots) + (size_t)pos * d;
-#pragma unroll
-    for (int r = 0; r < kDownR; ++r) {
-        const int j = t.row0 + 16 * r + f;
-        if (j >= d) continue;
-        int sum = 0;
-#pragma unroll
-        for (int i = 0; i < kWaves; ++i) sum += s_red[r][i][p][f];
-        y[j] = (float)sum * (sh * scale[j]);
+// Super-tile of the shared block: sn weight tiles x sm token tiles with sn | nt and sm | mt, at most one
+// XCD's resident blocks, as square as possible.
+void super_shape(int mt, int nt, int most, int32_t* out) {
+    int best_n = 1, best_m = 1, best_score = -1;
+    for (int sm = 1; sm <= mt && sm <= most; ++sm) {
+        if (mt % sm) continue;
+        for (int sn = 1; sn <= nt && sn * sm <= most; ++sn) {
+            if (nt % sn) continue;
+            const int score = sn * sm * 64 - (sn + sm);
+            if (score > best_score) { best_score = score; best_n = sn; best_m = sm; }
+        }
     }
+    out[0] = best_n;
+    out[1] = best_m;
 }
 
-// Upper bound of a launch's tiles: sum_e ceil(n_e / 16) <= slots / 16 + buckets.
-long long tile_bound(const FfnI8Args& a, int nf_sh, int nf_e, int feat) {
+long long tiles_of(long long n, int per) { return (n + per - 1) / per; }
+
+template <bool kUp, class C>
+hipError_t launch_pass(const FfnI8Args& a, const I8Plan& plan, hipStream_t s) {
+    constexpr int feat = kUp ? C::kUpFeat : C::BM;
     const long long slots = (long long)a.T * a.K, buckets = std::min<long long>(std::min(a.N, a.C), slots);
-    const long long nt_sh = (nf_sh + feat - 1) / feat, nt_e = (nf_e + feat - 1) / feat;
-    return (a.Is > 0 ? (a.T + kTok - 1) / kTok * nt_sh : 0) + (slots / kTok + buckets) * (buckets > 0 ? nt_e : 0);
+    const long long nt_sh = tiles_of(kUp ? a.Is : a.d, feat), nt_e = tiles_of(kUp ? a.I : a.d, feat);
+    Job job{a, {1, 1}, kUp || !a.part ? 1 : plan.parts, plan.xcd};
+    // upper bound: sum_e ceil(n_e / BT) <= slots / BT + buckets; blocks past the live tiles exit
+    const long long tiles = (a.Is > 0 ? tiles_of(a.T, C::BT) * nt_sh * job.parts : 0) +
+                            (buckets > 0 ? (slots / C::BT + buckets) * nt_e : 0);
+    if (tiles == 0) return hipSuccess;
+    if (tiles > 0x7FFFFFFFll) return hipErrorInvalidValue;
+    if (a.Is > 0 && plan.xcd) super_shape((int)tiles_of(a.T, C::BT), (int)nt_sh, C::kXcdBlocks, job.super);
+    hipLaunchKernelGGL((i8_gemm_kernel<kUp, C>), dim3((unsigned)tiles), dim3(C::kThreads), C::S * C::kStage, s, job);
+    return hipGetLastError();
+}
+
+hipError_t launch_quant(const FfnI8Args& a, int group, hipStream_t s) {
+    const long long nsh = a.Is > 0 ? a.T : 0, slots = a.C > 0 ? (long long)a.T * a.K : 0;
+    const long long segs_sh = (a.Is + kQuantRow - 1) / kQuantRow, segs = (a.I + kQuantRow - 1) / kQuantRow;
+    const long long blocks = nsh * segs_sh + slots * segs;
+    if (blocks > 0x7FFFFFFFll) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(i8_quant_kernel, dim3((unsigned)blocks), dim3(kQuantThreads), 0, s, a, (int)nsh, (int)segs_sh, (int)segs,
+                       group);
+    return hipGetLastError();
+}
+
+template <class C>
+hipError_t launch_all(const FfnI8Args& a, const I8Plan& plan, hipStream_t s) {
+    hipError_t e = launch_pass<true, C>(a, plan, s);
+    if (e == hipSuccess) e = launch_quant(a, C::kTopGroup, s);
+    return e == hipSuccess ? launch_pass<false, C>(a, plan, s) : e;
 }
 
 }  // namespace
 
 hipError_t launch_expert_ffn_i8(const FfnI8Args& a, hipStream_t s) {
-    const long long up = tile_bound(a, a.Is, a.I, 16), down = tile_bound(a, a.d, a.d, 16 * kDownR);
-    const long long rows = (a.Is > 0 ? a.T : 0) + (a.C > 0 ? (long long)a.T * a.K : 0);
-    if (rows == 0) return hipSuccess;
-    if (std::max({up, down, rows}) > 0x7FFFFFFFll) return hipErrorInvalidValue;
-    const bool gemm = expert_gemm_i8_applies(a);
-    hipError_t e = hipSuccess;
-    if (gemm) e = launch_expert_gemm_i8(a, true, s);
-    else hipLaunchKernelGGL(i8_up_kernel, dim3((unsigned)up), dim3(kThreads), 0, s, a);
-    hipLaunchKernelGGL(i8_quant_kernel, dim3((unsigned)rows), dim3(kThreads), 0, s, a);
-    if (e == hipSuccess && gemm) e = launch_expert_gemm_i8(a, false, s);
-    else if (!gemm) hipLaunchKernelGGL(i8_down_kernel, dim3((unsigned)down), dim3(kThreads), 0, s, a);
-    return e == hipSuccess ? hipGetLastError() : e;
+    if (a.Is <= 0 && a.C <= 0) return hipSuccess;
+    const I8Plan plan = i8_plan(a.T, a.d, a.N, a.K, a.C, a.I, a.Is);
+    switch (plan.shape) {
+        case 0: return launch_all<Tile64x32>(a, plan, s);
+        case 1: return launch_all<Tile64x64>(a, plan, s);
+        case 2: return launch_all<Tile128x64>(a, plan, s);
+        case 3: return launch_all<Tile128x128>(a, plan, s);
+        default: return launch_all<Tile256x256>(a, plan, s);
+    }
 }
 
 }  // namespace spice

@@ -179,12 +179,20 @@ WsLayout ws_layout(const spice_moe_cfg_t& c, int32_t T) {
     L.hqs = off;    off += i8 ? align256(t * i8_row(c.shared_inter)) : 0;
     L.hscale = off;   off += i8 ? align256(slots * sizeof(float)) : 0;
     L.hscale_s = off; off += i8 ? align256(t * sizeof(float)) : 0;
+    L.top = off;    off += i8 ? align256(slots * (size_t)c.inter / 16 * sizeof(float)) : 0;
+    L.top_s = off;  off += i8 ? align256(t * (size_t)c.shared_inter / 16 * sizeof(float)) : 0;
     L.base = off;
     L.zpart = off;
     if (T >= kRouteTiledMinT) {
         const size_t groups = (t + kRouteTileTok - 1) / kRouteTileTok;
         const int zp = route_parts(T, c.n_experts, c.d, c.dtype, SIZE_MAX);
         if (zp > 1) off += align256((size_t)zp * groups * kRouteTileTok * c.n_experts * sizeof(double));
+    }
+    if (i8) {
+        L.part = off;
+        off += align256(i8_part_bytes(i8_plan(T, c.d, c.n_experts, c.top_k, c.n_slots, c.inter, c.shared_inter), T, c.d));
+        L.total = off;
+        return L;
     }
     const int parts = c.dtype == SPICE_BF16 ? gemm_shared_parts(T, c.d, c.n_experts, c.top_k, c.n_slots, c.inter,
                                                                 c.shared_inter) : 1;

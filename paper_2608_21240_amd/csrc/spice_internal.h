@@ -5,6 +5,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "spice_moe.h"
 
 namespace spice {
@@ -79,7 +81,8 @@ struct WsLayout {
     size_t sgate;   // output gate of the shared block, fp32 [T]
     // 8-bit experts (SPICE_WFMT_INT8; h and hs are fp32 there): the requantised intermediates, int8
     // [T*K][i8_row(I)] and [T][i8_row(I_s)], and their scales, fp32 [T*K] and [T]
-    size_t hq, hqs, hscale, hscale_s;
+    // with a partial maximum per 16 values of the fp32 rows, fp32
+    size_t hq, hqs, hscale, hscale_s, top, top_s;
     size_t base;    // bytes every call needs; the rest is used when the workspace has it
     size_t zpart;   // partial logits of the tiled routing, fp64 (its own: no FFN buffer is touched by a routing call)
     size_t part;    // the shared block's partial results, fp32 [parts][T][d]
@@ -198,6 +201,57 @@ struct SpecArgs {
     float* h_conf;
 };
 
+// Tile shapes of the 8-bit expert FFN, smallest first: weight rows, tokens, bytes of LDS.
+struct I8Shape {
+    int rows, tokens, lds;
+};
+constexpr I8Shape kI8Shapes[5] = {{64, 32, 49152}, {64, 64, 49152}, {128, 64, 73728}, {128, 128, 65536}, {256, 256, 131072}};
+
+// How a call of the 8-bit expert FFN runs.
+// shape: by the mean bucket n = T K / N, since a tile as tall as the buckets are long reads each weight
+//   once; then smaller ones until the up launch has kI8MinTiles blocks.  us per call, shapes 0 .. 4:
+//   DeepSeek-V2-Lite sizes, 48 of 64 experts resident, T = 64 (n = 6) 92 / 96 / 98 / 109 / 133, T = 219
+//   (n = 20) 112 / 110 / 109 / 117 / 145, T = 400 (n = 37) 148 / 130 / 122 / 127 / 149, T = 1000 (n = 94)
+//   270 / 200 / 197 / 158 / 174, all resident T = 2000 612 / 413 / 410 / 324 / 289; Qwen2 sizes T = 64
+//   379 / 371 / 384 / 435 / 536, T = 500 932 / 727 / 693 / 580 / 670, T = 4096 5028 / 4100 / 3649 / 2754 / 2157.
+//   d = 512, 16 experts of 256, shared 512, T = 1000 (n = 125, 48 blocks of shape 4) 26 / 23 / 23 / 25 / 42.
+// parts: splits of the shared block's down contraction where its tiles would outlast the routed ones (Qwen2,
+//   T = 1 105 -> 88 us; T = 8, whose routed tiles take as long, 246 / 247), of 16 stages at least, as long
+//   as the GPU holds their blocks at once and their sums take 16 MiB at most.
+// xcd: whether neighbouring tiles, which share operands, run on one XCD: for the longest buckets only
+//   (Qwen2, T = 4096 2157 -> 2109 us), as the round robin spreads the weight stream (T = 32 343 / 396).
+struct I8Plan {
+    int shape, parts, xcd;
+};
+constexpr int kI8MinTiles = 400, kI8MaxParts = 8;
+// Arrival counters of the split tiles, in the control region.
+constexpr int kWordI8Parts = kWordSlotKeys + kRouteTokenMaxT * 64, kI8PartTiles = 4096;
+static_assert((kWordI8Parts + kI8PartTiles) * 4 <= SPICE_WS_CONTROL_BYTES, "control region too small");
+inline I8Plan i8_plan(int32_t T, int32_t d, int32_t N, int32_t K, int32_t C, int32_t I, int32_t Is) {
+    const int64_t n = (int64_t)T * K / (N > 0 ? N : 1), buckets = N < C ? N : C;
+    I8Plan p{};
+    p.shape = n < 10 ? 0 : n < 28 ? 1 : n < 48 ? 2 : n < 110 ? 3 : 4;
+    for (; p.shape > 0; --p.shape) {
+        const int64_t feat = kI8Shapes[p.shape].rows / 2, tok = kI8Shapes[p.shape].tokens;
+        const int64_t up = ((T + tok - 1) / tok) * ((Is + feat - 1) / feat) + buckets * ((n + tok - 1) / tok) * ((I + feat - 1) / feat);
+        if (up >= kI8MinTiles) break;
+    }
+    const I8Shape& s = kI8Shapes[p.shape];
+    const int64_t tiles = (int64_t)((T + s.tokens - 1) / s.tokens) * ((d + s.rows - 1) / s.rows);
+    const int64_t resident = 256 * (163840 / s.lds), room = (16 << 20) / ((int64_t)s.rows * s.tokens * 4);
+    const int64_t routed = std::min((int64_t)T * K, buckets) * ((d + s.rows - 1) / s.rows) * I / resident;
+    int64_t parts = 2 * routed < Is ? std::min<int64_t>({Is / 2048, resident / tiles, room / tiles, kI8MaxParts}) : 1;
+    p.parts = parts < 1 || tiles > kI8PartTiles ? 1 : (int)parts;
+    p.xcd = n >= 384;
+    return p;
+}
+// Bytes of the split tiles' partial sums.
+inline size_t i8_part_bytes(const I8Plan& p, int32_t T, int32_t d) {
+    const I8Shape& s = kI8Shapes[p.shape];
+    if (p.parts <= 1) return 0;
+    return (size_t)p.parts * ((T + s.tokens - 1) / s.tokens) * ((d + s.rows - 1) / s.rows) * s.rows * s.tokens * 4;
+}
+
 // The 8-bit expert FFN (expert_ffn_i8.hip).
 struct FfnI8Args {
     int32_t T, d, N, K, C, I, Is;
@@ -217,8 +271,11 @@ struct FfnI8Args {
     float* hs;              // workspace [T][I_s]
     int8_t* hq;             // workspace [T*K][i8_row(I)]
     int8_t* hqs;            // workspace [T][i8_row(I_s)]
+    float* top;             // workspace [T*K][I / 16]: partial maxima of a row of H
+    float* top_s;           // workspace [T][I_s / 16]
     float* hscale;          // workspace [T*K]
     float* hscale_s;        // workspace [T]
+    int32_t* part;          // workspace, partial sums of split tiles, or null: nothing is split
     uint32_t* ctrl;
 };
 
@@ -368,10 +425,6 @@ hipError_t launch_shared_gate(const void* x, const void* w_sg, int32_t T, int32_
 hipError_t launch_expert_ffn_fetched(const FfnArgs& a, const FetchArgs& f, hipStream_t s);
 hipError_t launch_combine(const CombineArgs& a, hipStream_t s);
 hipError_t launch_expert_ffn_i8(const FfnI8Args& a, hipStream_t s);
-// Its up or down products as GEMM tiles (expert_gemm_i8.hip), for many tokens.
-constexpr int kI8GemmMinTokens = 64;
-bool expert_gemm_i8_applies(const FfnI8Args& a);
-hipError_t launch_expert_gemm_i8(const FfnI8Args& a, bool up, hipStream_t s);
 hipError_t launch_rmsnorm_quant(const NormArgs& a, hipStream_t s);
 hipError_t launch_spec_update(const SpecArgs& a, hipStream_t s);
 
