@@ -64,7 +64,7 @@ extern "C" spice_status_t moe_rmsnorm_quant(const spice_moe_cfg_t* cfg, int32_t 
                     return fail(SPICE_ERR_INVALID, fn, "outputs overlap");
         }
         spice::NormArgs a{};
-        a.T = T; a.d = cfg->d; a.dtype = cfg->dtype; a.eps = eps;
+        a.T = T; a.d = cfg->d; a.dtype = cfg->dtype; a.eps = eps; a.inv_d = 1.0 / cfg->d;
         a.x = x; a.resid = resid; a.weight = weight; a.h = h_out; a.y = y_out; a.q = q_out; a.q_scale = q_scale;
         return hip_result(spice::launch_rmsnorm_quant(a, stream), fn);
     } catch (const std::exception& ex) {

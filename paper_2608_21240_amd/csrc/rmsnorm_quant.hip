@@ -20,6 +20,8 @@ struct Row;
 template <>
 struct Row<SPICE_BF16> {
     static constexpr int V = 8;  // elements per 16 bytes
+    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+    typedef float f32x2_t __attribute__((ext_vector_type(2)));
     __device__ static void widen(const uint4& q, double (&v)[8]) {
         const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
@@ -28,18 +30,14 @@ struct Row<SPICE_BF16> {
             v[2 * i + 1] = (double)__uint_as_float(w[i] & 0xFFFF0000u);
         }
     }
-    __device__ static uint32_t rne(double x) {
-        const uint32_t u = __float_as_uint((float)x);
-        if ((u & 0x7FFFFFFFu) > 0x7F800000u) return 0x7FC0u;
-        return (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
-    }
     __device__ static uint4 pack(const double (&v)[8]) {
-        uint4 q;
-        q.x = rne(v[0]) | (rne(v[1]) << 16);
-        q.y = rne(v[2]) | (rne(v[3]) << 16);
-        q.z = rne(v[4]) | (rne(v[5]) << 16);
-        q.w = rne(v[6]) | (rne(v[7]) << 16);
-        return q;
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {  // round to nearest even in one instruction
+            const f32x2_t f = {(float)v[2 * i], (float)v[2 * i + 1]};
+            w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2_t));
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
     }
 };
 
@@ -58,127 +56,130 @@ struct Row<SPICE_F32> {
     }
 };
 
-constexpr int kNormThreads = 256;
-constexpr int kNormChunks = 4;  // 16-byte chunks of a row per thread: rows of at most 16 KiB
-
-// One block per row.
-template <int DT>
-__global__ __launch_bounds__(kNormThreads) void rmsnorm_quant_kernel(NormArgs a) {
+// One 16-byte chunk of a row per thread: rows of more than 64 chunks take a block each (kWaveRows false),
+// shorter ones `lanes` lanes of a wave, a power of two.
+template <int DT, bool kWaveRows>
+__global__ __launch_bounds__(kWaveRows ? 256 : 1024) void rmsnorm_quant_kernel(NormArgs a, int lanes) {
     using R = Row<DT>;
-    constexpr int V = R::V, NW = kNormThreads / 64;
-    __shared__ double s_part[NW][3];
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const size_t row = blockIdx.x;
-    const int nc = a.d / V;
-    const uint4* x = static_cast<const uint4*>(a.x) + row * nc;
-    const uint4* r = a.resid ? static_cast<const uint4*>(a.resid) + row * nc : nullptr;
-    const uint4* wt = static_cast<const uint4*>(a.weight);
-    uint4 xv[kNormChunks], rv[kNormChunks], wv[kNormChunks];
+    constexpr int V = R::V;
+    const int nc = a.d / V, tid = threadIdx.x;
+    const size_t row = kWaveRows ? (size_t)blockIdx.x * (256 / lanes) + tid / lanes : blockIdx.x;
+    const int i = kWaveRows ? tid & (lanes - 1) : tid;
+    if (kWaveRows && row >= (size_t)a.T) return;  // whole groups of lanes
+    const bool in = i < nc;
+    const size_t at = row * nc + (in ? i : 0);
+    const uint4 zero = {0u, 0u, 0u, 0u};
+    uint4 xv = static_cast<const uint4*>(a.x)[at], rv = zero, wv = zero;
+    if (a.resid) rv = static_cast<const uint4*>(a.resid)[at];
+    if (a.weight) wv = static_cast<const uint4*>(a.weight)[in ? i : 0];
+    double s[V], p[V];  // s and s * w
+    R::widen(in ? xv : zero, s);
+    if (a.resid) {
+        double r[V];
+        R::widen(in ? rv : zero, r);
 #pragma unroll
-    for (int c = 0; c < kNormChunks; ++c) {
-        const int i = c * kNormThreads + tid;
-        const uint4 zero = {0u, 0u, 0u, 0u};
-        xv[c] = rv[c] = wv[c] = zero;
-        if (i < nc) {
-            xv[c] = x[i];
-            if (r) rv[c] = r[i];
-            if (wt) wv[c] = wt[i];
-        }
+        for (int k = 0; k < V; ++k) s[k] += r[k];
     }
-    auto load = [&](int c, double (&s)[V], double (&p)[V]) {  // s and s * w
-        double rr[V], ww[V];
-        R::widen(xv[c], s);
-        R::widen(rv[c], rr);
-        R::widen(wv[c], ww);
+    if (a.weight) {
+        double w[V];
+        R::widen(wv, w);
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-            if (r) s[k] += rr[k];
-            p[k] = wt ? s[k] * ww[k] : s[k];
-        }
-    };
+        for (int k = 0; k < V; ++k) p[k] = s[k] * w[k];
+    } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k) p[k] = s[k];
+    }
     double ss = 0.0, top = 0.0, bad = 0.0;  // bad: NaN once a product is not finite
 #pragma unroll
-    for (int c = 0; c < kNormChunks; ++c) {
-        if (c * kNormThreads >= nc) break;  // uniform
-        double s[V], p[V];
-        load(c, s, p);
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-            ss = fma(s[k], s[k], ss);
-            top = fmax(top, fabs(p[k]));
-            bad = fma(p[k], 0.0, bad);
-        }
+    for (int k = 0; k < V; ++k) {
+        ss = fma(s[k], s[k], ss);
+        top = fmax(top, fabs(p[k]));
+        bad = fma(p[k], 0.0, bad);
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
+    for (int o = (kWaveRows ? lanes : 64) / 2; o > 0; o >>= 1) {
         ss += __shfl_xor(ss, o);
         top = fmax(top, __shfl_xor(top, o));
-        bad += __shfl_xor(bad, o);
     }
-    if (lane == 0) {
-        s_part[w][0] = ss;
-        s_part[w][1] = top;
-        s_part[w][2] = bad;
+    bool nan = __ballot(bad != bad) != 0;
+    if constexpr (kWaveRows) {
+        const unsigned long long mine = lanes == 64 ? ~0ull : ((1ull << lanes) - 1) << ((tid & 63) & ~(lanes - 1));
+        nan = (__ballot(bad != bad) & mine) != 0;
+    } else {
+        __shared__ double s_part[16][2];
+        __shared__ int s_nan[16];
+        const int nw = (int)(blockDim.x >> 6), w = tid >> 6;
+        if ((tid & 63) == 0) {
+            s_part[w][0] = ss;
+            s_part[w][1] = top;
+            s_nan[w] = nan;
+        }
+        __syncthreads();
+        ss = top = 0.0;
+        int any = 0;
+        for (int k = 0; k < nw; ++k) {
+            ss += s_part[k][0];
+            top = fmax(top, s_part[k][1]);
+            any |= s_nan[k];
+        }
+        nan = any != 0;
     }
-    __syncthreads();
-    ss = s_part[0][0];
-    top = s_part[0][1];
-    bad = s_part[0][2];
-#pragma unroll
-    for (int i = 1; i < NW; ++i) {
-        ss += s_part[i][0];
-        top = fmax(top, s_part[i][1]);
-        bad += s_part[i][2];
-    }
-    const double rstd = ss == 0.0 ? 0.0 : 1.0 / sqrt(ss / a.d + a.eps);
-    const bool nan = bad != bad;
-    const double inv = nan || top == 0.0 ? 0.0 : 127.0 / top;
-    if (a.q && tid == 0) a.q_scale[row] = nan ? __builtin_nanf("") : (float)(top * rstd / 127.0);
-#pragma unroll
-    for (int c = 0; c < kNormChunks; ++c) {
-        const int i = c * kNormThreads + tid;
-        if (i >= nc) break;
-        double s[V], p[V], y[V];
-        load(c, s, p);
-        if (a.h) static_cast<uint4*>(a.h)[row * nc + i] = R::pack(s);
+    const double rstd = ss == 0.0 ? 0.0 : rsqrt(fma(ss, a.inv_d, a.eps));
+    if (a.q && i == 0) a.q_scale[row] = nan ? __builtin_nanf("") : (float)(top * rstd / 127.0);
+    if (!in) return;
+    if (a.h) static_cast<uint4*>(a.h)[at] = R::pack(s);
+    if (a.y) {
+        double y[V];
 #pragma unroll
         for (int k = 0; k < V; ++k) y[k] = p[k] * rstd;
-        if (a.y) static_cast<uint4*>(a.y)[row * nc + i] = R::pack(y);
-        if (a.q) {
-            // p * (127 / max) is off by a few units in the last place: where that can decide between two
-            // codes (bf16 rows hold exact halves), the one rounding of 127 p / max does
-            int q[V];
-            bool near = false;
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-                const double v = nan ? 0.0 : p[k] * inv, n = rint(v);
-                near |= fabs(fabs(v - n) - 0.5) < 1e-9;
-                q[k] = (int)n;
-            }
-            if (near) {
-#pragma unroll
-                for (int k = 0; k < V; ++k) q[k] = (int)rint(127.0 * p[k] / top);
-            }
-            uint32_t b[V / 4];
-#pragma unroll
-            for (int k = 0; k < V / 4; ++k)
-                b[k] = (uint32_t)(q[4 * k] & 255) | (uint32_t)(q[4 * k + 1] & 255) << 8 |
-                       (uint32_t)(q[4 * k + 2] & 255) << 16 | (uint32_t)(q[4 * k + 3] & 255) << 24;
-            uint32_t* out = reinterpret_cast<uint32_t*>(a.q + row * a.d) + (size_t)i * (V / 4);
-            if constexpr (V == 8) *reinterpret_cast<uint2*>(out) = make_uint2(b[0], b[1]);
-            else *out = b[0];
-        }
+        static_cast<uint4*>(a.y)[at] = R::pack(y);
     }
+    if (!a.q) return;
+    // p * (127 / max) is off by a few units in the last place: where that can decide between two codes (bf16
+    // rows hold exact halves), the one rounding of 127 p / max does
+    double inv = __builtin_amdgcn_rcp(top);  // and a step of Newton's: within 1e-15
+    inv = top > 0.0 ? 127.0 * fma(fma(-top, inv, 1.0), inv, inv) : 0.0;
+    int q[V];
+    bool near = false;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        const double v = p[k] * inv, n = rint(v);
+        near |= fabs(v - n) > 0.5 - 1e-9;
+        q[k] = (int)n;
+    }
+    if (near) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) q[k] = (int)rint(127.0 * p[k] / top);
+    }
+    uint32_t b[V / 4];
+#pragma unroll
+    for (int k = 0; k < V / 4; ++k)
+        b[k] = nan ? 0u
+                   : (uint32_t)(q[4 * k] & 255) | (uint32_t)(q[4 * k + 1] & 255) << 8 | (uint32_t)(q[4 * k + 2] & 255) << 16 |
+                         (uint32_t)q[4 * k + 3] << 24;
+    uint32_t* out = reinterpret_cast<uint32_t*>(a.q + row * a.d) + (size_t)i * (V / 4);
+    if constexpr (V == 8) *reinterpret_cast<uint2*>(out) = make_uint2(b[0], b[1]);
+    else *out = b[0];
+}
+
+template <int DT>
+hipError_t launch_norm(const NormArgs& a, hipStream_t s) {
+    const int nc = a.d / Row<DT>::V;
+    if (nc > 64) {
+        hipLaunchKernelGGL((rmsnorm_quant_kernel<DT, false>), dim3((unsigned)a.T), dim3((nc + 63) / 64 * 64), 0, s, a, 64);
+    } else {
+        int lanes = 1;
+        while (lanes < nc) lanes *= 2;
+        const int rows = 256 / lanes;
+        hipLaunchKernelGGL((rmsnorm_quant_kernel<DT, true>), dim3((unsigned)((a.T + rows - 1) / rows)), dim3(256), 0, s, a,
+                           lanes);
+    }
+    return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_rmsnorm_quant(const NormArgs& a, hipStream_t s) {
-    if (a.dtype == SPICE_BF16)
-        hipLaunchKernelGGL(rmsnorm_quant_kernel<SPICE_BF16>, dim3((unsigned)a.T), dim3(kNormThreads), 0, s, a);
-    else
-        hipLaunchKernelGGL(rmsnorm_quant_kernel<SPICE_F32>, dim3((unsigned)a.T), dim3(kNormThreads), 0, s, a);
-    return hipGetLastError();
+    return a.dtype == SPICE_BF16 ? launch_norm<SPICE_BF16>(a, s) : launch_norm<SPICE_F32>(a, s);
 }
 
 }  // namespace spice

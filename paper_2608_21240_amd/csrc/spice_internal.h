@@ -282,7 +282,7 @@ struct FfnI8Args {
 // RMS norm with the residual's addition and 8-bit output (rmsnorm_quant.hip).
 struct NormArgs {
     int32_t T, d, dtype;
-    double eps;
+    double eps, inv_d;   // 1 / d
     const void* x;
     const void* resid;   // nullable
     const void* weight;  // nullable

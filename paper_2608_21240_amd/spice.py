@@ -159,8 +159,9 @@ def _p(a):
         return None
     if isinstance(a, int):
         return a
-    if hasattr(a, "data_ptr"):
-        return a.data_ptr()
+    data_ptr = getattr(a, "data_ptr", None)
+    if data_ptr is not None:
+        return data_ptr()
     if hasattr(a, "ctypes"):
         return a.ctypes.data
     if isinstance(a, ctypes.Array):
@@ -168,11 +169,21 @@ def _p(a):
     raise TypeError(f"cannot pass {type(a).__name__} as a buffer")
 
 
-def _stream(s):
-    if s is None:
-        import torch
+_current_stream = None  # reads torch's current stream, once there is a GPU
 
-        return torch.cuda.current_stream().cuda_stream if torch.cuda.is_available() else None
+
+def _stream(s):
+    global _current_stream
+    if s is None:
+        if _current_stream is None:
+            import torch
+
+            if not torch.cuda.is_available():
+                return None
+            torch.cuda.init()
+            raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), torch.cuda.current_device
+            _current_stream = (lambda: raw(device())) if raw else (lambda: torch.cuda.current_stream().cuda_stream)
+        return _current_stream()
     if isinstance(s, int):
         return s
     return s.cuda_stream
