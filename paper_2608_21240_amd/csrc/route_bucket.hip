@@ -29,6 +29,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "route_device.h"
 
@@ -44,7 +45,7 @@ constexpr size_t kLogitLdsBytes = sizeof(TopkLds) > bucket_lds_bytes(kLogitThrea
 
 typedef double f64x4_t __attribute__((ext_vector_type(4)));
 
-template <int DT, bool kScored>
+template <int DT>
 __global__ __launch_bounds__(kLogitThreads) void route_logits_kernel(RouteArgs a, int g_per_tok) {
     __shared__ __align__(16) int s_lds[kLogitLdsBytes / sizeof(int)];
     __shared__ int s_flag;
@@ -53,12 +54,38 @@ __global__ __launch_bounds__(kLogitThreads) void route_logits_kernel(RouteArgs a
     const int n_rows = a.N + (a.w_sg ? 1 : 0);
     route_logits_rows<DT>(a, t, g * rows, min(n_rows, (g + 1) * rows));
     if (!route_last_block(&a.ctrl[kWordTokCount + t * kTokCountStride], g_per_tok, &s_flag)) return;
-    block_topk<kLogitThreads, true, true, kScored>(a, t, a.logits_ws + (size_t)t * a.N, *reinterpret_cast<TopkLds*>(s_lds));
+    block_topk<kLogitThreads, true, true>(a, t, a.logits_ws + (size_t)t * a.N, *reinterpret_cast<TopkLds*>(s_lds));
     // the published top-K outputs and keys of every token are at the device-coherent level
     // once every token's last block has counted itself here
     if (!route_last_block(&a.ctrl[kWordRouteDone], a.T, &s_flag)) return;
     bucket_slots<kLogitThreads, kBucketCache, true>(a, s_lds);
     if (a.hx || a.h_idx || a.h_w || a.h_cls || a.h_ready) mirror_host<kLogitThreads, true>(a);
+}
+
+// The same by a scoring rule, with more rows per block (kRows per wave): fewer blocks wait on a token's
+// counter, and more waves share the ranks.
+constexpr int kScoredThreads = 512;
+constexpr size_t kScoredLdsBytes =
+    std::max({sizeof(ScoredLds), sizeof(FewLds), bucket_lds_bytes(kLogitThreads, SPICE_MAX_EXPERTS, kBucketCache)});
+template <int DT, int kRows>
+__global__ __launch_bounds__(kScoredThreads) void route_scored_kernel(RouteArgs a, int g_per_tok) {
+    __shared__ __align__(16) int s_lds[kScoredLdsBytes / sizeof(int)];
+    __shared__ int s_flag;
+    const int t = blockIdx.x / g_per_tok, g = blockIdx.x % g_per_tok;
+    const int rows = (kScoredThreads / 64) * kRows;
+    route_logits_rows<DT, kRows>(a, t, g * rows, min(a.N, (g + 1) * rows));
+    if (!route_last_block(&a.ctrl[kWordTokCount + t * kTokCountStride], g_per_tok, &s_flag)) return;
+    block_topk_scored<kScoredThreads>(a, t, a.logits_ws + (size_t)t * a.N, *reinterpret_cast<ScoredLds*>(s_lds));
+    if (!route_last_block(&a.ctrl[kWordRouteDone], a.T, &s_flag)) return;
+    const bool copies = a.hx || a.h_idx || a.h_w || a.h_cls || a.h_ready;
+    if (a.T * a.K <= kFewSlots) {
+        bucket_few_slots<kScoredThreads>(a, *reinterpret_cast<FewLds*>(s_lds));
+        if (copies) mirror_host<kScoredThreads, true>(a);
+        return;
+    }
+    if (threadIdx.x >= kLogitThreads) return;  // ended waves are not waited for
+    bucket_slots<kLogitThreads, kBucketCache, true>(a, s_lds);
+    if (copies) mirror_host<kLogitThreads, true>(a);
 }
 
 constexpr int kPrefillThreads = 1024;  // 16 waves
@@ -251,8 +278,9 @@ __global__ __launch_bounds__(kPrefillThreads) void route_tiled_kernel(RouteArgs 
         if constexpr (kScored) {
             // the partial logits are summed: their region holds the waves' group values
             static_assert(sizeof(GroupLds) * kNW <= sizeof(L.zp), "group values fit the partial logits' region");
-            score_experts<WaveTeam>(a, L.z[tt], L.key[tt], reinterpret_cast<GroupLds*>(L.zp)[w]);
-            WaveTeam::sync();
+            wave_topk_scored(a, L.z[tt], reinterpret_cast<double*>(L.key[tt]), reinterpret_cast<GroupLds*>(L.zp)[w],
+                             L.pick[tt]);
+            continue;
         }
 #pragma unroll
         for (int j = 0; j < kJ; ++j) {
@@ -445,13 +473,30 @@ __global__ __launch_bounds__(64) void bucket_scatter_kernel(RouteArgs a) {
 
 namespace {
 
+template <int DT>
+hipError_t launch_scored_rows(const RouteArgs& a, hipStream_t s) {
+    auto launch = [&](auto rows) {
+        constexpr int kRows = decltype(rows)::value, per = kScoredThreads / 64 * kRows;
+        const int g = (a.N + per - 1) / per;
+        hipLaunchKernelGGL((route_scored_kernel<DT, kRows>), dim3((unsigned)(a.T * g)), dim3(kScoredThreads), 0, s, a, g);
+        return hipGetLastError();
+    };
+    // Rows per wave: more read a token's x once for several rows and leave fewer blocks, fewer shorten the
+    // way to a token's last block.  1 / 2 / 4, us per call: N = 64, T = 1 9.2 / 9.6 / 11.2, T = 128 16.1 /
+    // 14.1 / 14.9; N = 256, T = 16 20.5 / 18.7 / 21.1, T = 48 34.9 / 32.7 / 32.9, T = 128 67.7 / 56.2 / 44.4.
+    const int64_t rows = (int64_t)a.T * a.N;
+    return rows < 3000 ? launch(std::integral_constant<int, 1>{})
+                       : rows < 16000 ? launch(std::integral_constant<int, 2>{}) : launch(std::integral_constant<int, 4>{});
+}
+
 template <int DT, bool kScored>
 hipError_t launch_route(const RouteArgs& a, hipStream_t s) {
     const unsigned groups = (unsigned)((a.T + kPrefillTok - 1) / kPrefillTok);
     const int parts = route_parts(a.T, a.N, a.d, a.dtype, a.part_bytes);
     if (route_keeps_rows(a.T, a.N, a.d, parts, a.hx != nullptr)) {
+        if constexpr (kScored) return launch_scored_rows<DT>(a, s);
         const int g = route_blocks_per_token(a.N + (a.w_sg ? 1 : 0), kLogitThreads);
-        hipLaunchKernelGGL((route_logits_kernel<DT, kScored>), dim3((unsigned)(a.T * g)), dim3(kLogitThreads), 0, s, a, g);
+        hipLaunchKernelGGL(route_logits_kernel<DT>, dim3((unsigned)(a.T * g)), dim3(kLogitThreads), 0, s, a, g);
         return hipGetLastError();
     }
     const dim3 grid(groups * (unsigned)parts);
