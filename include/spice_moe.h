@@ -305,7 +305,7 @@ spice_status_t moe_expert_ffn_grouped_gated(const spice_moe_cfg_t* cfg, int32_t 
  *                 NULL without them
  *   w13_pool, w2_pool, w13_shared, w2_shared  device blobs (see SPICE_WFMT_INT8)
  *   w_shared_gate device [d] bf16, or NULL: as in moe_expert_ffn_grouped_gated
- *   lore_A, lore_B  as in lore_surrogate_apply (whose launches follow when both are given), or NULL
+ *   lore_A, lore_B  as in lore_surrogate_apply, whose corrections run in the same launches, or NULL
  *   perm, offsets, resident_slot, y_slots, y_shared, ws  as in moe_expert_ffn_grouped
  * Errors: as moe_expert_ffn_grouped, plus UNSUPPORTED for another wfmt or unaligned buffers (16 bytes).
  */

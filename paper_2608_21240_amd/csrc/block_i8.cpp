@@ -83,7 +83,7 @@ extern "C" spice_status_t moe_expert_ffn_grouped_i8(const spice_moe_cfg_t* cfg, 
                                                     float* y_shared, void* ws, size_t ws_bytes, spice_stream_t stream) {
     const char* fn = "moe_expert_ffn_grouped_i8";
     try {
-        spice_status_t st = spice::validate(cfg, T);
+        const spice_status_t st = spice::validate(cfg, T);
         if (st != SPICE_OK) return st;
         const spice_moe_cfg_t& c = *cfg;
         if (c.wfmt != SPICE_WFMT_INT8) return fail(SPICE_ERR_UNSUPPORTED, fn, "needs SPICE_WFMT_INT8 expert weights");
@@ -101,8 +101,9 @@ extern "C" spice_status_t moe_expert_ffn_grouped_i8(const spice_moe_cfg_t* cfg, 
         for (const auto& n : need)
             if (n.needed && !n.p) return fail(SPICE_ERR_INVALID, fn, std::string(n.name) + " is NULL");
         if (!aligned16(x_q) || !aligned16(w13_pool) || !aligned16(w2_pool) || !aligned16(y_slots) || !aligned16(y_shared) ||
-            (shared && (!aligned16(w13_shared) || !aligned16(w2_shared))))
-            return fail(SPICE_ERR_UNSUPPORTED, fn, "x_q, weights and outputs must be 16-byte aligned");
+            (shared && (!aligned16(w13_shared) || !aligned16(w2_shared))) ||
+            (lore && (!aligned16(x) || !aligned16(lore_A) || !aligned16(lore_B))))
+            return fail(SPICE_ERR_UNSUPPORTED, fn, "activations, weights and outputs must be 16-byte aligned");
         const spice::WsLayout L = spice::ws_layout(c, T);
         if (ws_bytes < L.base)
             return fail(SPICE_ERR_WORKSPACE, fn, "workspace has " + std::to_string(ws_bytes) + " bytes, needs " +
@@ -134,9 +135,13 @@ extern "C" spice_status_t moe_expert_ffn_grouped_i8(const spice_moe_cfg_t* cfg, 
             if (e != hipSuccess) return hip_result(e, fn);
             a.sgate = sg;
         }
-        st = hip_result(spice::launch_expert_ffn_i8(a, stream), fn);
-        if (st != SPICE_OK || !lore || c.lore_rank == 0) return st;
-        return lore_surrogate_apply(cfg, T, x, perm, offsets, lore_A, lore_B, y_slots, ws, ws_bytes, stream);
+        if (lore && c.lore_rank > 0) {
+            a.r = c.lore_rank;
+            a.x = static_cast<const uint16_t*>(x);
+            a.lore_A = static_cast<const uint16_t*>(lore_A); a.lore_B = static_cast<const uint16_t*>(lore_B);
+            a.u = reinterpret_cast<float*>(wsb + L.u);
+        }
+        return hip_result(spice::launch_expert_ffn_i8(a, stream), fn);
     } catch (const std::exception& ex) {
         return spice::set_error(SPICE_ERR_INTERNAL, ex.what());
     } catch (...) {

@@ -15,6 +15,9 @@
 // sub-tiles are interleaved with the other waves' (rows kTStride t + 16 wt), so the ragged last tile of an
 // expert spreads over the SIMDs; sub-tiles without a live token are not read and issue no MFMA, and their
 // rows are not fetched.
+// The LoRE corrections of the LORE buckets (Eq. 9) run beside them: U = A_e x of a bucket is a tile of the
+// up launch on the same stages with bf16 MFMAs, U B_e^T one of the down launch; they come first, since an
+// up tile's bf16 rows are twice as long (block of 16 tokens 97 -> 84 us).
 // Staging: buffer loads straight to LDS into a ring of S stages of 128-byte rows whose 16-byte chunks are
 // XOR-swizzled by row (chunk c of row r at c ^ ((r >> 1) & 7)).  A chunk past the end of a row, and a row
 // past the end of a matrix or a bucket, reads zero (an offset past the buffer).
@@ -23,7 +26,9 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
+#include "lore_tile.h"
 #include "route_last.h"
 #include "spice_internal.h"
 
@@ -69,6 +74,7 @@ constexpr int kRawBufferWord3 = 0x00020000;      // gfx9 raw buffer: 32-bit data
 
 typedef int i32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ float silu(float u) { return u / (1.0f + __expf(-u)); }
 
@@ -89,14 +95,16 @@ struct Job {
     FfnI8Args a;
     int32_t super[2];  // shared-block super-tile (weight tiles, token tiles)
     int32_t parts;     // splits of the shared block's down contraction
+    int32_t lore;      // first blocks of the launch, which take the LORE tiles (a bound)
     int32_t xcd;       // whether neighbouring tiles run on one XCD
 };
 
 struct Tile {
-    bool shared;
-    const char* w;        // the matrix's blob
+    bool shared, lore;
+    const void* w;        // the matrix's blob (A_e or B_e of a LORE tile)
     uint32_t w_bytes;     // of its codes
-    int kdim, nfeat;      // contraction, output features
+    int kdim, nfeat;      // bytes of a row (the contraction, but for a LORE tile), output features
+    int up_off;           // up: rows from a tile row of the first half to its partner of the second
     int row0;             // first feature
     int tok0, ntok;       // first token of the tile in its group, tokens of the group
     int start;            // the group's first bucket position (0 for the shared block)
@@ -105,15 +113,18 @@ struct Tile {
     int part;             // and which part of it
 };
 
-// The HIT bucket holding tile L of nt tiles per token tile, by a wave's scan of the offsets.
-__device__ bool find_bucket(const FfnI8Args& a, int nt, int BT, int& L, int lane, int& e_, int& st_, int& n_) {
-    const int32_t* off = a.offsets + SPICE_CLASS_HIT * (a.N + 1);
+// The bucket of class c holding tile L of nt tiles per token tile, by a wave's scan of the offsets; slot:
+// its pool slot (class HIT).
+__device__ bool find_bucket(const FfnI8Args& a, int c, int nt, int BT, int& L, int lane, int& e_, int& st_, int& n_,
+                            int& slot_) {
+    const int32_t* off = a.offsets + c * (a.N + 1);
     for (int e0 = 0; e0 < a.N; e0 += 64) {
         const int e = e0 + lane;
-        int st = 0, n = 0;
+        int st = 0, n = 0, slot = -1;
         if (e < a.N) {
             st = off[e];
             n = off[e + 1] - st;
+            if (c == SPICE_CLASS_HIT) slot = a.resident_slot[e];
         }
         if (n > a.T * a.K) n = 0;
         const int tiles = n > 0 ? ((n + BT - 1) / BT) * nt : 0;
@@ -130,6 +141,7 @@ __device__ bool find_bucket(const FfnI8Args& a, int nt, int BT, int& L, int lane
             e_ = e0 + src;
             st_ = __builtin_amdgcn_readlane(st, src);
             n_ = __builtin_amdgcn_readlane(n, src);
+            slot_ = __builtin_amdgcn_readlane(slot, src);
             L -= __builtin_amdgcn_readlane(excl, src);
             return true;
         }
@@ -138,57 +150,75 @@ __device__ bool find_bucket(const FfnI8Args& a, int nt, int BT, int& L, int lane
     return false;
 }
 
-// Logical tile L of a launch (every wave resolves it for itself): the shared block's tiles first, in
-// groups of about an XCD's blocks that share operand tiles in its L2, then the HIT buckets in id order,
-// the token tiles of one weight tile next to each other.
+// Logical tile L of a launch (every wave resolves it for itself): the LORE tiles in the first job.lore
+// blocks, then the shared block's, in groups of about an XCD's blocks that share operand tiles in its L2,
+// then the HIT buckets in id order, the token tiles of one weight tile next to each other.
 template <bool kUp, class C>
 __device__ bool resolve(const Job& job, int L, Tile& j) {
     const FfnI8Args& a = job.a;
     constexpr int feat = kUp ? C::kUpFeat : C::BM;
-    const int nt_sh = ((kUp ? a.Is : a.d) + feat - 1) / feat, nt_e = ((kUp ? a.I : a.d) + feat - 1) / feat;
-    const int mt_sh = (a.T + C::BT - 1) / C::BT;
-    const int parts = kUp ? 1 : job.parts, per_part = nt_sh * mt_sh;
-    const int tiles_sh = a.Is > 0 ? per_part * parts : 0;
     j.k0 = 0;
     j.split = -1;
     j.part = 0;
-    if (L < tiles_sh) {
-        j.part = L / per_part;
-        L -= j.part * per_part;
-        if (parts > 1) j.split = L;
-        const int sn = job.super[0], sm = job.super[1];
-        const int g = L / (sn * sm), in = L - g * (sn * sm), mg = mt_sh / sm;
-        j.shared = true;
-        j.w = kUp ? a.w13s : a.w2s;
-        j.w_bytes = (uint32_t)(kUp ? 2 : 1) * (uint32_t)a.Is * (uint32_t)a.d;
-        j.kdim = kUp ? a.d : a.Is;
-        j.nfeat = kUp ? a.Is : a.d;
-        j.row0 = ((g / mg) * sn + in / sm) * feat;
-        j.tok0 = ((g % mg) * sm + in % sm) * C::BT;
-        j.ntok = a.T;
-        j.start = 0;
-        const int nk = (j.kdim + kBK - 1) / kBK;
-        j.k0 = j.part * nk / parts;
-        j.k1 = (j.part + 1) * nk / parts;
-        return true;
+    j.shared = j.lore = false;
+    int e = 0, st = 0, n = 0, slot = -1;
+    const int lane = threadIdx.x & 63;
+    if (L < job.lore) {
+        constexpr int rows = kUp ? C::BM : C::BM * kLoreDown;
+        const int nt = ((kUp ? a.r : a.d) + rows - 1) / rows;
+        if (!find_bucket(a, SPICE_CLASS_LORE, nt, C::BT, L, lane, e, st, n, slot)) return false;
+        j.lore = true;
+        j.w = (kUp ? a.lore_A : a.lore_B) + (size_t)e * a.r * a.d;
+        j.w_bytes = (uint32_t)a.r * (uint32_t)a.d * 2u;
+        j.kdim = kUp ? 2 * a.d : 2 * a.r;
+        j.nfeat = kUp ? a.r : a.d;
+        j.up_off = C::kUpFeat;  // BM consecutive rows of A
+    } else {
+        L -= job.lore;
+        const int nt_sh = ((kUp ? a.Is : a.d) + feat - 1) / feat, nt_e = ((kUp ? a.I : a.d) + feat - 1) / feat;
+        const int mt_sh = (a.T + C::BT - 1) / C::BT;
+        const int parts = kUp ? 1 : job.parts, per_part = nt_sh * mt_sh;
+        const int tiles_sh = a.Is > 0 ? per_part * parts : 0;
+        if (L < tiles_sh) {
+            j.part = L / per_part;
+            L -= j.part * per_part;
+            if (parts > 1) j.split = L;
+            const int sn = job.super[0], sm = job.super[1];
+            const int g = L / (sn * sm), in = L - g * (sn * sm), mg = mt_sh / sm;
+            j.shared = true;
+            j.w = kUp ? a.w13s : a.w2s;
+            j.w_bytes = (uint32_t)(kUp ? 2 : 1) * (uint32_t)a.Is * (uint32_t)a.d;
+            j.kdim = kUp ? a.d : a.Is;
+            j.nfeat = kUp ? a.Is : a.d;
+            j.up_off = j.nfeat;
+            j.row0 = ((g / mg) * sn + in / sm) * feat;
+            j.tok0 = ((g % mg) * sm + in % sm) * C::BT;
+            j.ntok = a.T;
+            j.start = 0;
+            const int nk = (j.kdim + kBK - 1) / kBK;
+            j.k0 = j.part * nk / parts;
+            j.k1 = (j.part + 1) * nk / parts;
+            return true;
+        }
+        L -= tiles_sh;
+        if (a.C <= 0 || !find_bucket(a, SPICE_CLASS_HIT, nt_e, C::BT, L, lane, e, st, n, slot)) return false;
+        if (slot < 0 || slot >= a.C) {
+            if (threadIdx.x == 0) atomicOr(&a.ctrl[kWordFlags], (uint32_t)SPICE_FLAG_BAD_SLOT);
+            return false;
+        }
+        const size_t elems = (size_t)(kUp ? 2 : 1) * a.I * a.d, rows = kUp ? 2 * (size_t)a.I : (size_t)a.d;
+        j.w = (kUp ? a.w13_pool : a.w2_pool) + (size_t)slot * (elems + 4 * rows);
+        j.w_bytes = (uint32_t)elems;
+        j.kdim = kUp ? a.d : a.I;
+        j.nfeat = kUp ? a.I : a.d;
+        j.up_off = j.nfeat;
     }
-    L -= tiles_sh;
-    int e = 0, st = 0, n = 0;
-    if (a.C <= 0 || !find_bucket(a, nt_e, C::BT, L, threadIdx.x & 63, e, st, n)) return false;
-    const int slot = a.resident_slot[e];
-    if (st < 0 || st + n > a.T * a.K || slot < 0 || slot >= a.C) {
-        if (threadIdx.x == 0)
-            atomicOr(&a.ctrl[kWordFlags], (uint32_t)(slot < 0 || slot >= a.C ? SPICE_FLAG_BAD_SLOT : SPICE_FLAG_BAD_INDEX));
+    if (st < 0 || st + n > a.T * a.K) {
+        if (threadIdx.x == 0) atomicOr(&a.ctrl[kWordFlags], (uint32_t)SPICE_FLAG_BAD_INDEX);
         return false;
     }
     const int mt = (n + C::BT - 1) / C::BT, nn = L / mt;
-    const size_t elems = (size_t)(kUp ? 2 : 1) * a.I * a.d, rows = kUp ? 2 * (size_t)a.I : (size_t)a.d;
-    j.shared = false;
-    j.w = (kUp ? a.w13_pool : a.w2_pool) + (size_t)slot * (elems + 4 * rows);
-    j.w_bytes = (uint32_t)elems;
-    j.kdim = kUp ? a.d : a.I;
-    j.nfeat = kUp ? a.I : a.d;
-    j.row0 = nn * feat;
+    j.row0 = nn * (!j.lore ? feat : kUp ? C::BM : C::BM * kLoreDown);
     j.tok0 = (L - nn * mt) * C::BT;
     j.ntok = n;
     j.start = st;
@@ -232,8 +262,8 @@ struct Frags {
 };
 
 // The main loop of one tile with NL live token sub-tiles in this wave (NL = 0: the wave only loads and
-// keeps the barriers).
-template <class C, bool kUp, int NL, class Load>
+// keeps the barriers).  kBf16: rows of bf16, 64 k per stage.
+template <class C, bool kUp, bool kBf16, int NL, class Load>
 __device__ __forceinline__ void product(unsigned char* s_lds, int nk, uint32_t fbase, uint32_t tbase, Load load,
                                         i32x4_t (&acc)[C::RF][C::RT]) {
     constexpr int N1 = NL > 0 ? NL : 1;
@@ -257,8 +287,15 @@ __device__ __forceinline__ void product(unsigned char* s_lds, int nk, uint32_t f
 #pragma unroll
             for (int t = 0; t < NL; ++t)
 #pragma unroll
-                for (int s = 0; s < C::RF; ++s)
-                    acc[s][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(f.a[s], f.b[t], acc[s][t], 0, 0, 0);
+                for (int s = 0; s < C::RF; ++s) {
+                    if constexpr (kBf16)  // a LORE tile's sums are fp32, in the same registers
+                        acc[s][t] = __builtin_bit_cast(
+                            i32x4_t, __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                                         __builtin_bit_cast(bf16x8_t, f.a[s]), __builtin_bit_cast(bf16x8_t, f.b[t]),
+                                         __builtin_bit_cast(f32x4_t, acc[s][t]), 0, 0, 0));
+                    else
+                        acc[s][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(f.a[s], f.b[t], acc[s][t], 0, 0, 0);
+                }
             __builtin_amdgcn_s_setprio(0);
         }
     };
@@ -329,6 +366,12 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2))
     Tile j;
     __shared__ int s_last;
     if (!resolve<kUp, C>(job, job.xcd ? xcd_tile(blockIdx.x, gridDim.x, C::kXcdBlocks) : (int)blockIdx.x, j)) return;
+    if constexpr (!kUp) {
+        if (j.lore) {
+            for (int b = 0; b < kLoreDown && j.row0 < a.d; ++b, j.row0 += C::BM) lore_down<C>(a, j);
+            return;
+        }
+    }
     const int tid = threadIdx.x, lane = tid & 63;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wf = w % C::WF, wt = w / C::WF;  // wave's feature part and token lane group
@@ -348,11 +391,11 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2))
     const int r0 = tid / 8;
     const bool loader = C::kLoaders == C::kThreads || tid < C::kLoaders;
     const int c16 = (int)((lds_off(r0, tid & 7) & 127u) >> 4);
-    const uint32_t ldx = kUp ? (uint32_t)a.d : (uint32_t)i8_row(j.kdim);
-    // up: all tokens' rows (512 MiB at most); down: the tile's, which are consecutive
+    const uint32_t ldx = kUp ? (uint32_t)j.kdim : (uint32_t)i8_row(j.kdim);
+    // up: all tokens' rows (1 GiB at most); down: the tile's, which are consecutive
     const size_t row_first = (size_t)j.start + j.tok0;
     const rsrc_t wbuf = raw_buffer(j.w, j.w_bytes);
-    const rsrc_t xbuf = kUp ? raw_buffer(a.xq, (uint32_t)a.T * ldx)
+    const rsrc_t xbuf = kUp ? raw_buffer(j.lore ? static_cast<const void*>(a.x) : a.xq, (uint32_t)a.T * ldx)
                             : raw_buffer((j.shared ? a.hqs : a.hq) + row_first * ldx, (uint32_t)min(C::BT, j.ntok - j.tok0) * ldx);
     const uint32_t wstep = (uint32_t)j.kdim;
     const uint32_t woff0 = (uint32_t)(j.row0 + r0) * wstep + c16 * 16;
@@ -371,7 +414,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2))
 #pragma unroll
         for (int i = 0; i < C::kWLoads; ++i) {
             const int r = C::kRowStep * i;
-            const uint32_t delta = (uint32_t)(kUp && r >= C::kUpFeat ? j.nfeat + r - C::kUpFeat : r) * wstep;
+            const uint32_t delta = (uint32_t)(kUp && r >= C::kUpFeat ? j.up_off + r - C::kUpFeat : r) * wstep;
             load_lds16(wbuf, in ? woff0 + delta + (uint32_t)kt * kBK : kOutOfRange, run + i * C::kRowStep * 128);
         }
     };
@@ -417,15 +460,36 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2))
     const uint32_t fbase = lds_off(frow0 + m, quad);
     const uint32_t tbase = C::kWTile + lds_off(wt * 16 + m, quad);
     static_assert(C::RT == 1 || C::RT == 2 || C::RT == 4, "token sub-tiles per wave");
-    if (nlive == C::RT) product<C, kUp, C::RT>(s_lds, nk, fbase, tbase, load, acc);
-    else if (nlive == 0) product<C, kUp, 0>(s_lds, nk, fbase, tbase, load, acc);
-    else if constexpr (C::RT > 2) {
-        if (nlive == 1) product<C, kUp, 1>(s_lds, nk, fbase, tbase, load, acc);
-        else if (nlive == 2) product<C, kUp, 2>(s_lds, nk, fbase, tbase, load, acc);
-        else product<C, kUp, 3>(s_lds, nk, fbase, tbase, load, acc);
-    } else if constexpr (C::RT > 1) {
-        product<C, kUp, 1>(s_lds, nk, fbase, tbase, load, acc);
+    auto multiply = [&](auto bf16) {
+        constexpr bool kBf16 = decltype(bf16)::value;
+        if (nlive == C::RT) product<C, kUp, kBf16, C::RT>(s_lds, nk, fbase, tbase, load, acc);
+        else if (nlive == 0) product<C, kUp, kBf16, 0>(s_lds, nk, fbase, tbase, load, acc);
+        else if constexpr (C::RT > 2) {
+            if (nlive == 1) product<C, kUp, kBf16, 1>(s_lds, nk, fbase, tbase, load, acc);
+            else if (nlive == 2) product<C, kUp, kBf16, 2>(s_lds, nk, fbase, tbase, load, acc);
+            else product<C, kUp, kBf16, 3>(s_lds, nk, fbase, tbase, load, acc);
+        } else if constexpr (C::RT > 1) {
+            product<C, kUp, kBf16, 1>(s_lds, nk, fbase, tbase, load, acc);
+        }
+    };
+    if constexpr (kUp) {
+        if (j.lore) {
+            multiply(std::true_type{});
+#pragma unroll
+            for (int t = 0; t < C::RT; ++t) {
+                const int p = j.tok0 + t * C::kTStride + wt * 16 + m;
+                if (p >= j.ntok) continue;
+                float* dst = a.u + (size_t)(j.start + p) * a.r;
+#pragma unroll
+                for (int s = 0; s < C::RF; ++s) {
+                    const int q = j.row0 + frow0 + (s % (C::RF / 2)) * 16 + (s / (C::RF / 2)) * C::kUpFeat + quad * 4;
+                    if (q < a.r) *reinterpret_cast<i32x4_t*>(dst + q) = acc[s][t];
+                }
+            }
+            return;
+        }
     }
+    multiply(std::false_type{});
 
     if constexpr (!kUp) {
         if (j.split >= 0) {
@@ -436,7 +500,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2))
     }
 
     // Epilogue: lane holds features 4 quad .. + 3 of sub-tile s for token m of sub-tile t.
-    const float* scale = reinterpret_cast<const float*>(j.w + j.w_bytes);
+    const float* scale = reinterpret_cast<const float*>(static_cast<const char*>(j.w) + j.w_bytes);
 #pragma unroll
     for (int t = 0; t < C::RT; ++t) {
         const int p = j.tok0 + t * C::kTStride + wt * 16 + m;
@@ -554,12 +618,15 @@ hipError_t launch_pass(const FfnI8Args& a, const I8Plan& plan, hipStream_t s) {
     constexpr int feat = kUp ? C::kUpFeat : C::BM;
     const long long slots = (long long)a.T * a.K, buckets = std::min<long long>(std::min(a.N, a.C), slots);
     const long long nt_sh = tiles_of(kUp ? a.Is : a.d, feat), nt_e = tiles_of(kUp ? a.I : a.d, feat);
-    Job job{a, {1, 1}, kUp || !a.part ? 1 : plan.parts, plan.xcd};
+    Job job{a, {1, 1}, kUp || !a.part ? 1 : plan.parts, 0, plan.xcd};
+    const long long lore_b = a.r > 0 ? std::min<long long>(a.N, slots) : 0;
+    const long long lore = lore_b ? (slots / C::BT + lore_b) * tiles_of(kUp ? a.r : a.d, kUp ? C::BM : C::BM * kLoreDown) : 0;
     // upper bound: sum_e ceil(n_e / BT) <= slots / BT + buckets; blocks past the live tiles exit
     const long long tiles = (a.Is > 0 ? tiles_of(a.T, C::BT) * nt_sh * job.parts : 0) +
-                            (buckets > 0 ? (slots / C::BT + buckets) * nt_e : 0);
+                            (buckets > 0 ? (slots / C::BT + buckets) * nt_e : 0) + lore;
     if (tiles == 0) return hipSuccess;
     if (tiles > 0x7FFFFFFFll) return hipErrorInvalidValue;
+    job.lore = (int32_t)lore;
     if (a.Is > 0 && plan.xcd) super_shape((int)tiles_of(a.T, C::BT), (int)nt_sh, C::kXcdBlocks, job.super);
     hipLaunchKernelGGL((i8_gemm_kernel<kUp, C>), dim3((unsigned)tiles), dim3(C::kThreads), C::S * C::kStage, s, job);
     return hipGetLastError();
@@ -570,6 +637,7 @@ hipError_t launch_quant(const FfnI8Args& a, int group, hipStream_t s) {
     const long long segs_sh = (a.Is + kQuantRow - 1) / kQuantRow, segs = (a.I + kQuantRow - 1) / kQuantRow;
     const long long blocks = nsh * segs_sh + slots * segs;
     if (blocks > 0x7FFFFFFFll) return hipErrorInvalidValue;
+    if (blocks == 0) return hipSuccess;
     hipLaunchKernelGGL(i8_quant_kernel, dim3((unsigned)blocks), dim3(kQuantThreads), 0, s, a, (int)nsh, (int)segs_sh, (int)segs,
                        group);
     return hipGetLastError();
@@ -585,7 +653,6 @@ hipError_t launch_all(const FfnI8Args& a, const I8Plan& plan, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_expert_ffn_i8(const FfnI8Args& a, hipStream_t s) {
-    if (a.Is <= 0 && a.C <= 0) return hipSuccess;
     const I8Plan plan = i8_plan(a.T, a.d, a.N, a.K, a.C, a.I, a.Is);
     switch (plan.shape) {
         case 0: return launch_all<Tile64x32>(a, plan, s);

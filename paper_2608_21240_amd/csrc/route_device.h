@@ -394,7 +394,7 @@ __device__ void block_topk_scored(const RouteArgs& a, int t, const double* zg, S
 
 // The same by one wave: z = the token's N logits in, its scores out; c = its choice values; pick = its K
 // experts (all in LDS).
-__device__ void wave_topk_scored(const RouteArgs& a, double* z, double* c, GroupLds& G, int* pick) {
+__device__ inline void wave_topk_scored(const RouteArgs& a, double* z, double* c, GroupLds& G, int* pick) {
     constexpr int kJ = SPICE_MAX_EXPERTS / 64;
     const int N = a.N, lane = threadIdx.x & 63;
     auto sync = [] {  // a wave's LDS accesses complete in order; only the compiler has to keep theirs

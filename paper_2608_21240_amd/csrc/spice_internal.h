@@ -276,6 +276,12 @@ struct FfnI8Args {
     float* hscale;          // workspace [T*K]
     float* hscale_s;        // workspace [T]
     int32_t* part;          // workspace, partial sums of split tiles, or null: nothing is split
+    // the LoRE corrections of the LORE buckets, with r > 0
+    int32_t r;
+    const uint16_t* x;      // bf16 activations
+    const uint16_t* lore_A;
+    const uint16_t* lore_B;
+    float* u;               // workspace [T*K][r]
     uint32_t* ctrl;
 };
 
