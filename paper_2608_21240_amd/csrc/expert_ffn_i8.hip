@@ -213,7 +213,7 @@ __device__ bool resolve(const Job& job, int L, Tile& j) {
         j.nfeat = kUp ? a.I : a.d;
         j.up_off = j.nfeat;
     }
-    if (st < 0 || st + n > a.T * a.K) {
+    if (st < 0 || st > a.T * a.K - n) {
         if (threadIdx.x == 0) atomicOr(&a.ctrl[kWordFlags], (uint32_t)SPICE_FLAG_BAD_INDEX);
         return false;
     }
@@ -442,6 +442,37 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2))
         sid[i] = -1;
         if (loader && pos < j.ntok) sid[i] = !kUp ? pos - j.tok0 : j.shared ? pos : a.perm[j.start + pos];
     }
+    // What the epilogue needs is on its way before the ring's first loads (a wait by count then waits for
+    // it too): the scales of the wave's weight rows and of its tokens, else one or two trips to memory at
+    // the end of a short tile.
+    constexpr bool kEarly = C::RF <= 4;  // registers: the scales of a 256-row tile are loaded late
+    const float* scales = reinterpret_cast<const float*>(static_cast<const char*>(j.w) + j.w_bytes);
+    auto row_scale = [&](int s) {
+        const int f = j.row0 + frow0 + (kUp ? s % (C::RF / 2) : s) * 16 + quad * 4;
+        return *reinterpret_cast<const f32x4_t*>(scales + (f < j.nfeat ? f : 0) + (kUp && s >= C::RF / 2 ? j.nfeat : 0));
+    };
+    auto row_id = [&](int t) {
+        const int p = min(j.tok0 + t * C::kTStride + wt * 16 + m, j.ntok - 1);
+        return !kUp || j.shared ? p : a.perm[j.start + p];
+    };
+    auto row_factor = [&](int id) {
+        if constexpr (kUp) {
+            return a.xs[j.shared ? id : slot_token(a, id)];
+        } else {
+            const size_t pos = (size_t)j.start + id;
+            return (j.shared ? a.hscale_s : a.hscale)[pos] * (j.shared && a.sgate ? a.sgate[pos] : 1.f);
+        }
+    };
+    f32x4_t sc[C::RF];
+    int rid[C::RT];
+    float factor[C::RT];
+    if constexpr (kEarly) {
+#pragma unroll
+        for (int s = 0; s < C::RF; ++s)
+            if (!j.lore) sc[s] = row_scale(s);
+#pragma unroll
+        for (int t = 0; t < C::RT; ++t) rid[t] = row_id(t);
+    }
     __builtin_amdgcn_sched_barrier(0);
     load_w(0, 0);
     __builtin_amdgcn_sched_barrier(0);
@@ -452,6 +483,10 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2))
         if (loader && pos < j.ntok) xoff[i] = (uint32_t)(!kUp || j.shared ? sid[i] : slot_token(a, sid[i])) * ldx + c16 * 16;
     }
     load_x(0, 0);
+    if constexpr (kEarly) {
+#pragma unroll
+        for (int t = 0; t < C::RT; ++t) factor[t] = row_factor(rid[t]);
+    }
 #pragma unroll
     for (int s = 1; s < C::S; ++s) load(s, s);
 
@@ -500,22 +535,20 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2))
     }
 
     // Epilogue: lane holds features 4 quad .. + 3 of sub-tile s for token m of sub-tile t.
-    const float* scale = reinterpret_cast<const float*>(static_cast<const char*>(j.w) + j.w_bytes);
 #pragma unroll
     for (int t = 0; t < C::RT; ++t) {
         const int p = j.tok0 + t * C::kTStride + wt * 16 + m;
         if (p >= j.ntok) continue;
         const size_t pos = (size_t)j.start + p;
         if constexpr (kUp) {
-            const float sx = a.xs[j.shared ? p : slot_token(a, a.perm[pos])];
+            const float sx = kEarly ? factor[t] : row_factor(row_id(t));
             float* dst = (j.shared ? a.hs : a.h) + pos * j.nfeat;
             float top = 0.f, bad = 0.f;  // bad: NaN once a value is not finite
 #pragma unroll
             for (int s = 0; s < C::RF / 2; ++s) {
                 const int f = j.row0 + frow0 + s * 16 + quad * 4;
                 if (f >= j.nfeat) continue;
-                const f32x4_t sg = *reinterpret_cast<const f32x4_t*>(scale + f);
-                const f32x4_t su = *reinterpret_cast<const f32x4_t*>(scale + j.nfeat + f);
+                const f32x4_t sg = kEarly ? sc[s] : row_scale(s), su = kEarly ? sc[s + C::RF / 2] : row_scale(s + C::RF / 2);
                 f32x4_t h;
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
@@ -534,17 +567,16 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2))
             const int f0 = j.row0 + frow0;
             if (quad == 0 && f0 < j.nfeat) (j.shared ? a.top_s : a.top)[pos * (j.nfeat / 16) + f0 / C::kTopGroup] = top;
         } else {
-            float sh = (j.shared ? a.hscale_s : a.hscale)[pos];
-            if (j.shared && a.sgate) sh *= a.sgate[pos];
+            const float sh = kEarly ? factor[t] : row_factor(row_id(t));
             float* dst = (j.shared ? a.y_shared : a.y_slots) + pos * a.d;
 #pragma unroll
             for (int s = 0; s < C::RF; ++s) {
                 const int f = j.row0 + frow0 + s * 16 + quad * 4;
                 if (f >= a.d) continue;
-                const f32x4_t sc = *reinterpret_cast<const f32x4_t*>(scale + f);
+                const f32x4_t s2 = kEarly ? sc[s] : row_scale(s);
                 f32x4_t y;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) y[i] = (float)acc[s][t][i] * (sh * sc[i]);
+                for (int i = 0; i < 4; ++i) y[i] = (float)acc[s][t][i] * (sh * s2[i]);
                 *reinterpret_cast<f32x4_t*>(dst + f) = y;
             }
         }
