@@ -150,6 +150,14 @@ __device__ bool find_bucket(const FfnI8Args& a, int c, int nt, int BT, int& L, i
     return false;
 }
 
+// Tile L of a matrix's nt weight tiles x mt token tiles: the token tiles of a weight tile are 8 blocks
+// apart, so they run on one XCD, one after the other, and read the weights once into its L2.
+__device__ __forceinline__ void spread(int L, int nt, int mt, int& w, int& t) {
+    const int g = L / (8 * mt), wide = min(8, nt - 8 * g), in = L - g * 8 * mt;
+    t = in / wide;
+    w = 8 * g + in - t * wide;
+}
+
 // Logical tile L of a launch (every wave resolves it for itself): the LORE tiles in the first job.lore
 // blocks, then the shared block's, in groups of about an XCD's blocks that share operand tiles in its L2,
 // then the HIT buckets in id order, the token tiles of one weight tile next to each other.
@@ -183,16 +191,22 @@ __device__ bool resolve(const Job& job, int L, Tile& j) {
             j.part = L / per_part;
             L -= j.part * per_part;
             if (parts > 1) j.split = L;
-            const int sn = job.super[0], sm = job.super[1];
-            const int g = L / (sn * sm), in = L - g * (sn * sm), mg = mt_sh / sm;
             j.shared = true;
             j.w = kUp ? a.w13s : a.w2s;
             j.w_bytes = (uint32_t)(kUp ? 2 : 1) * (uint32_t)a.Is * (uint32_t)a.d;
             j.kdim = kUp ? a.d : a.Is;
             j.nfeat = kUp ? a.Is : a.d;
             j.up_off = j.nfeat;
-            j.row0 = ((g / mg) * sn + in / sm) * feat;
-            j.tok0 = ((g % mg) * sm + in % sm) * C::BT;
+            if (job.xcd) {
+                const int sn = job.super[0], sm = job.super[1];
+                const int g = L / (sn * sm), in = L - g * (sn * sm), mg = mt_sh / sm;
+                j.row0 = ((g / mg) * sn + in / sm) * feat;
+                j.tok0 = ((g % mg) * sm + in % sm) * C::BT;
+            } else {
+                spread(L, nt_sh, mt_sh, j.row0, j.tok0);
+                j.row0 *= feat;
+                j.tok0 *= C::BT;
+            }
             j.ntok = a.T;
             j.start = 0;
             const int nk = (j.kdim + kBK - 1) / kBK;
@@ -217,9 +231,15 @@ __device__ bool resolve(const Job& job, int L, Tile& j) {
         if (threadIdx.x == 0) atomicOr(&a.ctrl[kWordFlags], (uint32_t)SPICE_FLAG_BAD_INDEX);
         return false;
     }
-    const int mt = (n + C::BT - 1) / C::BT, nn = L / mt;
-    j.row0 = nn * (!j.lore ? feat : kUp ? C::BM : C::BM * kLoreDown);
-    j.tok0 = (L - nn * mt) * C::BT;
+    const int mt = (n + C::BT - 1) / C::BT, rows = !j.lore ? feat : kUp ? C::BM : C::BM * kLoreDown;
+    if (job.xcd) {
+        j.row0 = L / mt * rows;
+        j.tok0 = L % mt * C::BT;
+    } else {
+        spread(L, (j.nfeat + rows - 1) / rows, mt, j.row0, j.tok0);
+        j.row0 *= rows;
+        j.tok0 *= C::BT;
+    }
     j.ntok = n;
     j.start = st;
     j.k1 = (j.kdim + kBK - 1) / kBK;
