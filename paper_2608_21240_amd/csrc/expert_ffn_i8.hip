@@ -56,7 +56,6 @@ struct Shape {
     static_assert((S - 1) * (kWLoads + kXLoads) < 64, "vmcnt holds the loads in flight");
 };
 using Tile64x32 = Shape<64, 32, 2, 2, 4, 4>;
-using Tile64x64 = Shape<64, 64, 2, 2, 3, 4>;
 using Tile128x64 = Shape<128, 64, 2, 2, 3, 4>;
 using Tile128x128 = Shape<128, 128, 2, 4, 2, 4>;
 using Tile256x256 = Shape<256, 256, 2, 4, 2, 4>;
@@ -64,8 +63,8 @@ template <class C>
 constexpr bool matches(const I8Shape& s) {
     return C::BM == s.rows && C::BT == s.tokens && C::S * C::kStage == s.lds;
 }
-static_assert(matches<Tile64x32>(kI8Shapes[0]) && matches<Tile64x64>(kI8Shapes[1]) && matches<Tile128x64>(kI8Shapes[2]) &&
-                  matches<Tile128x128>(kI8Shapes[3]) && matches<Tile256x256>(kI8Shapes[4]),
+static_assert(matches<Tile64x32>(kI8Shapes[0]) && matches<Tile128x64>(kI8Shapes[1]) && matches<Tile128x128>(kI8Shapes[2]) &&
+                  matches<Tile256x256>(kI8Shapes[3]),
               "the shapes as the rules know them");
 
 constexpr int kBK = 128;                         // contraction per stage
@@ -708,9 +707,8 @@ hipError_t launch_expert_ffn_i8(const FfnI8Args& a, hipStream_t s) {
     const I8Plan plan = i8_plan(a.T, a.d, a.N, a.K, a.C, a.I, a.Is);
     switch (plan.shape) {
         case 0: return launch_all<Tile64x32>(a, plan, s);
-        case 1: return launch_all<Tile64x64>(a, plan, s);
-        case 2: return launch_all<Tile128x64>(a, plan, s);
-        case 3: return launch_all<Tile128x128>(a, plan, s);
+        case 1: return launch_all<Tile128x64>(a, plan, s);
+        case 2: return launch_all<Tile128x128>(a, plan, s);
         default: return launch_all<Tile256x256>(a, plan, s);
     }
 }

@@ -205,36 +205,40 @@ struct SpecArgs {
 struct I8Shape {
     int rows, tokens, lds;
 };
-constexpr I8Shape kI8Shapes[5] = {{64, 32, 49152}, {64, 64, 49152}, {128, 64, 73728}, {128, 128, 65536}, {256, 256, 131072}};
+constexpr I8Shape kI8Shapes[4] = {{64, 32, 49152}, {128, 64, 73728}, {128, 128, 65536}, {256, 256, 131072}};
 
 // How a call of the 8-bit expert FFN runs.
 // shape: by the mean bucket n = T K / N, since a tile as tall as the buckets are long reads each weight
-//   once; then smaller ones until the up launch has kI8MinTiles blocks.  us per call, shapes 0 .. 4:
-//   DeepSeek-V2-Lite sizes, 48 of 64 experts resident, T = 64 (n = 6) 92 / 96 / 98 / 109 / 133, T = 219
-//   (n = 20) 112 / 110 / 109 / 117 / 145, T = 400 (n = 37) 148 / 130 / 122 / 127 / 149, T = 1000 (n = 94)
-//   270 / 200 / 197 / 158 / 174, all resident T = 2000 612 / 413 / 410 / 324 / 289; Qwen2 sizes T = 64
-//   379 / 371 / 384 / 435 / 536, T = 500 932 / 727 / 693 / 580 / 670, T = 4096 5028 / 4100 / 3649 / 2754 / 2157.
-//   d = 512, 16 experts of 256, shared 512, T = 1000 (n = 125, 48 blocks of shape 4) 26 / 23 / 23 / 25 / 42.
+//   once; then smaller ones until the up launch fills the CUs, which takes more blocks the taller they are.
+//   us per call, shapes 0 .. 3: DeepSeek-V2-Lite sizes, 48 of 64 experts resident, T = 64 (n = 6) 90 / 95 /
+//   109 / 134, T = 130 (n = 12) 98 / 96 / 111 / 138, T = 219 (n = 20) 107 / 99 / 116 / 148, T = 500 (n = 46)
+//   152 / 121 / 127 / 157, T = 700 (n = 65) 180 / 146 / 136 / 164, T = 1000 (n = 93) 231 / 169 / 151 / 176,
+//   all resident T = 2000 (n = 187) 490 / 329 / 296 / 289; Qwen2 sizes T = 300 (n = 37) 617 / 481 / 499 /
+//   620, T = 500 (n = 62) 824 / 594 / 558 / 669, T = 1000 (n = 125) 1418 / 895 / 771 / 769.  Small layers
+//   (d, experts, their inter, shared inter; up blocks): 1024, 8, 512, 1024, T = 500 26 (1024) / 22 (256) / 26
+//   (128) / 51 (32); 1024, 4, 1024, 1024, T = 1000 49 / 37 (768) / 34 (384) / 58 (96).
 // parts: splits of the shared block's down contraction where its tiles would outlast the routed ones (Qwen2,
 //   T = 1 105 -> 88 us; T = 8, whose routed tiles take as long, 246 / 247), of 16 stages at least, as long
 //   as the GPU holds their blocks at once and their sums take 16 MiB at most.
-// xcd: whether neighbouring tiles, which share operands, run on one XCD: for the longest buckets only
-//   (Qwen2, T = 4096 2157 -> 2109 us), as the round robin spreads the weight stream (T = 32 343 / 396).
+// xcd: whether an XCD's resident blocks take neighbouring tiles, a few weight tiles x a few token tiles,
+//   rather than the token tiles of single weight tiles: for the longest buckets only (no / yes:
+//   DeepSeek-V2-Lite T = 4096 (n = 384) 486 / 492, T = 8192 (n = 768) 917 / 892, Qwen2 T = 1000 769 / 872,
+//   T = 4096 (n = 512) 2127 / 2120).
 struct I8Plan {
     int shape, parts, xcd;
 };
-constexpr int kI8MinTiles = 400, kI8MaxParts = 8;
+constexpr int kI8MinTiles = 300, kI8MaxParts = 8;  // up blocks per 128 tokens of a tile's height
 // Arrival counters of the split tiles, in the control region.
 constexpr int kWordI8Parts = kWordSlotKeys + kRouteTokenMaxT * 64, kI8PartTiles = 4096;
 static_assert((kWordI8Parts + kI8PartTiles) * 4 <= SPICE_WS_CONTROL_BYTES, "control region too small");
 inline I8Plan i8_plan(int32_t T, int32_t d, int32_t N, int32_t K, int32_t C, int32_t I, int32_t Is) {
     const int64_t n = (int64_t)T * K / (N > 0 ? N : 1), buckets = N < C ? N : C;
     I8Plan p{};
-    p.shape = n < 10 ? 0 : n < 28 ? 1 : n < 48 ? 2 : n < 110 ? 3 : 4;
+    p.shape = n < 12 ? 0 : n < 52 ? 1 : n < 140 ? 2 : 3;
     for (; p.shape > 0; --p.shape) {
         const int64_t feat = kI8Shapes[p.shape].rows / 2, tok = kI8Shapes[p.shape].tokens;
         const int64_t up = ((T + tok - 1) / tok) * ((Is + feat - 1) / feat) + buckets * ((n + tok - 1) / tok) * ((I + feat - 1) / feat);
-        if (up >= kI8MinTiles) break;
+        if (up * 128 >= kI8MinTiles * tok) break;
     }
     const I8Shape& s = kI8Shapes[p.shape];
     const int64_t tiles = (int64_t)((T + s.tokens - 1) / s.tokens) * ((d + s.rows - 1) / s.rows);
@@ -242,7 +246,7 @@ inline I8Plan i8_plan(int32_t T, int32_t d, int32_t N, int32_t K, int32_t C, int
     const int64_t routed = std::min((int64_t)T * K, buckets) * ((d + s.rows - 1) / s.rows) * I / resident;
     int64_t parts = 2 * routed < Is ? std::min<int64_t>({Is / 2048, resident / tiles, room / tiles, kI8MaxParts}) : 1;
     p.parts = parts < 1 || tiles > kI8PartTiles ? 1 : (int)parts;
-    p.xcd = n >= 384;
+    p.xcd = n >= 512;
     return p;
 }
 // Bytes of the split tiles' partial sums.
