@@ -113,3 +113,14 @@ def swiglu_i8_ref(xq, xs, w13, w2, d, I):
 
 def lore_ref(x, A, B):
     return x.double() @ A.double().t() @ B.double().t()
+
+
+# Calls (T, d, N, K, I, Is, C) of the 8-bit experts and the tile shape that takes each: small contractions and
+# many features, so that a call is long enough for its shape and quick to check.
+SHAPE_CALLS = [
+    ((120, 48, 10, 1, 272, 144, 6), 0), ((400, 64, 64, 2, 128, 320, 64), 1), ((1000, 80, 36, 2, 528, 272, 30), 2),
+    ((2300, 64, 64, 4, 1296, 400, 64), 3), ((4200, 64, 32, 4, 1040, 400, 32), 3)]
+# Calls whose shared block's down contraction is split, with the parts, and one just too short for it.
+SPLIT_CALLS = [
+    ((1, 64, 4, 1, 16, 8192, 1), 4), ((70, 208, 4, 2, 32, 4112, 2), 2), ((3, 4096, 8, 2, 48, 16400, 8), 8),
+    ((500, 128, 4, 1, 64, 6160, 0), 3), ((1, 64, 4, 1, 16, 4080, 1), 1)]

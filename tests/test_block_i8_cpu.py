@@ -1,10 +1,15 @@
 """The 8-bit MoE block without a GPU: what its entry points refuse, its weight format in the host's
 residual, the cache and the layer generator."""
 import ctypes
+import os
+import random
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
 
+import block_i8 as R
 from paper_2608_21240_amd import spice, synth, workloads as W
 
 D = 0x100000  # never dereferenced: every call below fails validation first
@@ -180,3 +185,81 @@ def test_layer_driver_asks_for_the_norm():
     run.shape = S
     with pytest.raises(ValueError, match="separate calls"):
         run.layer_gpu(type("L", (), {"wfmt": 0})(), None, None)
+
+
+# ---- the rules that pick a call's kernels ------------------------------------------------------
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
+DSV2, QWEN2 = (2048, 64, 6, 1408, 2816), (3584, 64, 8, 2560, 20480)
+
+
+@pytest.fixture(scope="module")
+def plan(tmp_path_factory):
+    """plan(T, d, N, K, C, I, Is) -> (shape, parts, xcd, bytes of the parts' sums, rows, tokens)."""
+    if not shutil.which("g++") or not os.path.exists(os.path.join(ROCM, "include", "hip", "hip_runtime_api.h")):
+        pytest.skip("g++ or the HIP headers are not installed")
+    exe = str(tmp_path_factory.mktemp("plan") / "driver")
+    subprocess.run(["g++", "-std=c++17", "-O1", f"-I{ROOT}/include", f"-I{ROOT}/paper_2608_21240_amd/csrc",
+                    f"-I{ROCM}/include", "-D__HIP_PLATFORM_AMD__", os.path.join(ROOT, "tests", "i8_plan_driver.cpp"),
+                    "-o", exe], check=True)
+
+    def ask(*calls):
+        text = "".join(" ".join(map(str, c)) + "\n" for c in calls)
+        r = subprocess.run([exe], input=text, capture_output=True, text=True, check=True)
+        out = [tuple(map(int, ln.split())) for ln in r.stdout.splitlines()]
+        assert len(out) == len(calls)
+        return out
+
+    return ask
+
+
+def of(layer, T, C):
+    d, N, K, I, Is = layer
+    return (T, d, N, K, C, I, Is)
+
+
+@pytest.mark.parametrize("layer,T,C,shape", [
+    (DSV2, 1, 32, 0), (DSV2, 64, 48, 0), (DSV2, 219, 48, 1), (DSV2, 500, 48, 1), (DSV2, 700, 48, 2), (DSV2, 1000, 48, 2),
+    (DSV2, 2000, 64, 3), (QWEN2, 16, 64, 0), (QWEN2, 300, 64, 1), (QWEN2, 500, 64, 2), (QWEN2, 4096, 64, 3),
+    ((1024, 8, 2, 512, 1024), 500, 8, 1), ((1024, 4, 2, 1024, 1024), 1000, 4, 2), ((2048, 8, 2, 1024, 256), 700, 8, 1)])
+def test_tile_shapes(plan, layer, T, C, shape):
+    assert plan(of(layer, T, C))[0][0] == shape
+
+
+def test_neighbouring_tiles_share_an_xcd_in_the_longest_calls_only(plan):
+    got = plan(*[of(DSV2, T, 64) for T in (1, 1000, 4096, 5461, 5462, 8192)])
+    assert [g[2] for g in got] == [0, 0, 0, 0, 1, 1]  # from 512 tokens per expert
+
+
+def test_calls_of_each_shape_and_split(plan):
+    for (T, d, N, K, I, Is, C), shape in R.SHAPE_CALLS:
+        assert plan((T, d, N, K, C, I, Is))[0][0] == shape
+    T, d, N, K, I, Is, C = R.SHAPE_CALLS[-1][0]
+    assert plan((T, d, N, K, C, I, Is))[0][2] == 1
+    for (T, d, N, K, I, Is, C), parts in R.SPLIT_CALLS:
+        assert plan((T, d, N, K, C, I, Is))[0][1] == parts
+
+
+def test_plans_stay_within_their_limits(plan):
+    r = random.Random(3)
+    calls = []
+    for _ in range(4000):
+        N = r.randint(1, 256)
+        calls.append((int(2 ** r.uniform(0, 16)), 16 * r.randint(1, 512), N, r.randint(1, min(N, 64)), r.randint(0, N),
+                      16 * r.randint(1, 8191), 16 * r.randint(0, 8191)))
+    for (T, d, N, K, C, I, Is), (shape, parts, xcd, room, rows, tokens) in zip(calls, plan(*calls)):
+        tiles = -(-T // tokens) * -(-d // rows)
+        assert 0 <= shape <= 3 and 1 <= parts <= 8
+        if parts > 1:
+            # every part has work, its tile has a counter, and the sums have their room
+            assert parts * 2048 <= Is and tiles <= 4096 and room == parts * tiles * rows * tokens * 4 <= 16 << 20
+        else:
+            assert room == 0
+
+
+def test_the_workspace_has_the_split_tiles_sums(plan):
+    for (T, d, N, K, I, Is, C), parts in R.SPLIT_CALLS:
+        a, b = (spice.spice_workspace_bytes(cfg(W.MoEShape(d, N, K, I, s, 0, W.DTYPE_BF16), n_slots=C), T) for s in (Is, 16))
+        rows = T * ((Is - 16) * 4 + (Is - 16) // 16 * 4)  # H and its partial maxima
+        assert a - b >= rows + plan((T, d, N, K, C, I, Is))[0][3]

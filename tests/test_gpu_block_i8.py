@@ -226,6 +226,37 @@ def test_bad_logits_still_give_valid_experts(T):
         r.check_buckets()
 
 
+@pytest.mark.parametrize("T,N,K", [(13, 40, 5), (16, 40, 4), (64, 9, 1), (128, 256, 8), (207, 256, 2), (208, 16, 2)])
+def test_scored_routing_at_the_limits_of_its_variants(T, N, K):
+    """64 and 65 slots, 1, 2 and 4 rows per wave, the last and the first T of the row and tile forms."""
+    for rule in RULES:
+        r = Routing(T, 128, N, K, C=N // 2, seed=T)
+        if N % rule.get("groups", 1) or K > rule.get("keep", 1) * (N // rule.get("groups", 1)):
+            rule = dict(sigmoid=True)
+        r.run(**rule)
+        r.check(r.logits.cpu().numpy(), **rule)
+
+
+def test_scored_routing_of_many_tokens():
+    r = Routing(20000, 64, 16, 3, C=5, seed=3, norm_topk=1)
+    rule = dict(sigmoid=True, groups=4, keep=2, top=2, balance=True, scale=2.5)
+    r.run(**rule)
+    r.check(r.logits.cpu().numpy(), **rule)
+
+
+@pytest.mark.parametrize("T", [5, 300])
+def test_scored_routing_copies_to_the_host(T):
+    r = Routing(T, 64, 48, 5, C=9, seed=2)
+    pin = lambda t: torch.zeros(t.shape, dtype=t.dtype).pin_memory()  # noqa: E731
+    x, idx, w, cls = (pin(t) for t in (r.x, r.idx, r.w, r.cls))
+    counts, ready = (torch.zeros(n, dtype=torch.int32).pin_memory() for n in (4, 1))
+    r.run(sigmoid=True, groups=4, keep=2, host_out=spice.host_out(x, idx, w, cls, counts, ready, 77))
+    torch.cuda.synchronize()
+    for a, b in ((x, r.x), (idx, r.idx), (w, r.w), (cls, r.cls)):
+        assert torch.equal(a, b.cpu())
+    assert counts[:3].tolist() == torch.bincount(r.cls.flatten().long(), minlength=3).tolist() and ready.item() == 77
+
+
 @pytest.mark.parametrize("mode", [spice.SPICE_CONF_GATE, spice.SPICE_CONF_GATE_RENORM])
 @pytest.mark.parametrize("T,norm", [(9, 0), (9, 1), (300, 0)])
 def test_confidence_from_the_gates(mode, T, norm):
@@ -336,6 +367,51 @@ def test_experts(size, skew):
     e.check()
 
 
+@pytest.mark.parametrize("size", [s for s, _ in R.SHAPE_CALLS])
+def test_experts_in_each_tile_shape(size):
+    say("experts", size)
+    e = Experts(*size, seed=1, skew=size[0] > 2000)
+    e.run()
+    e.check()
+
+
+@pytest.mark.parametrize("size,parts", R.SPLIT_CALLS)
+def test_experts_with_a_split_shared_block(size, parts):
+    """The split's sums are whole numbers: the same bits with the workspace's optional end and without it, and
+    again on the same workspace (its counters are back at zero)."""
+    say("experts", size)
+    e = Experts(*size, seed=2)
+    e.run()
+    e.check()
+    want = e.y_slots.clone(), e.y_shared.clone()
+    for short in (0, 1, 0) if parts > 1 else (0,):
+        e.wsn -= short
+        e.run()
+        e.wsn += short
+        assert torch.equal(e.y_slots, want[0]) and torch.equal(e.y_shared, want[1])
+
+
+def test_split_experts_in_a_graph_beside_an_eager_call():
+    """Replays of a captured call, with calls of another workspace on another stream in between."""
+    a, b = (Experts(3, 256, 8, 2, 48, 8192, 8, seed=s) for s in (1, 2))
+    for e in (a, b):
+        e.run()
+    torch.cuda.synchronize()
+    want = [(e.y_slots.clone(), e.y_shared.clone()) for e in (a, b)]
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph):
+        a.run()
+    for _ in range(4):
+        for e in (a, b):
+            e.y_slots.fill_(7), e.y_shared.fill_(7)
+        side.wait_stream(torch.cuda.current_stream())
+        graph.replay()
+        b.run(stream=side)
+        torch.cuda.synchronize()
+        for e, w in zip((a, b), want):
+            assert torch.equal(e.y_slots, w[0]) and torch.equal(e.y_shared, w[1])
+
+
 @pytest.mark.parametrize("T", [1, 20, 150, 400])
 def test_experts_with_gate_and_surrogates(T):
     e = Experts(T, 256, 8, 3, 96, 160, 4, r=16, seed=T, lore=True)
@@ -386,6 +462,34 @@ def test_experts_bad_indices_raise_a_flag(T):
     e.offsets[0, 2:] += T * 2
     e.run()
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("T", [1, 60])
+def test_surrogates_of_every_rank_and_long_buckets(T):
+    """All misses are surrogates of one expert or of a few; ranks of one chunk and of several stages."""
+    for r, N in ((8, 2), (72, 3), (256, 5)):
+        e = Experts(T, 192, N, 1, 32, 48, 1, r=r, seed=r, skew=True, lore=True)
+        e.run(lore=True)
+        e.check(lore=True)
+
+
+def test_surrogates_with_bad_indices_raise_a_flag():
+    e = Experts(40, 64, 4, 2, 48, 32, 0, r=8, seed=3, lore=True)
+    e.perm[0], e.perm[1] = -5, 1000
+    e.run(lore=True)
+    assert spice.spice_workspace_flags(e.ws, e.wsn, clear=True) & spice.SPICE_FLAG_BAD_INDEX
+    e = Experts(40, 64, 4, 2, 48, 32, 0, r=8, seed=3, lore=True)
+    e.offsets[1, 2:] += 2 ** 30
+    e.run(lore=True)
+    torch.cuda.synchronize()
+
+
+def test_surrogates_alone_after_the_experts():
+    """The separate surrogate call takes the 8-bit layer's configuration: the corrections are the same."""
+    e = Experts(90, 256, 8, 3, 96, 160, 4, r=16, seed=7, lore=True)
+    e.run()
+    spice.lore_surrogate_apply(e.cfg, 90, e.x, e.perm, e.offsets, e.lore_A, e.lore_B, e.y_slots, e.ws, e.wsn)
+    e.check(lore=True)
 
 
 def test_experts_give_the_same_bits_each_time():
@@ -550,6 +654,24 @@ def test_layer_driver(T, gate):
             room[t] += g[t, k] * (tv + 16 * U * v.abs())
     room += ref.abs() * (2.0 ** -8 + 8 * U) + 16 * U * ref.abs().amax(1, keepdim=True)
     assert ((out.double() - ref).abs() <= room).all()
+
+
+@pytest.mark.parametrize("T", [5, 300])
+def test_layer_driver_with_a_scoring_rule_and_bf16_experts(T):
+    """The softmax rule without groups is the plain routing: the layer's output is the same bits."""
+    s = W.small_shape()
+    wl = W.Workload("s", s, tokens=T, resident=s.n_experts // 2, skew=False)
+    host = LY.HostLayer(wl)
+    x = torch.randn(T, s.d, generator=R.gen(1)).to(BF).cuda()
+    conf = torch.from_numpy(synth.gen_conf(wl)).cuda()
+    out = []
+    for score in (None, spice.route_score()):
+        dev = LY.DeviceLayer(host)
+        run = LY.LayerRun(s, T, dev.C, tau=wl.tau, layer_call=False, score=score)
+        out.append(run.forward(dev, x, conf).clone())
+        torch.cuda.synchronize()
+        assert run.flags() == 0
+    assert torch.equal(out[0], out[1])
 
 
 def test_cache_admits_8_bit_experts():
