@@ -23,6 +23,15 @@
 // past the end of a matrix or a bucket, reads zero (an offset past the buffer).
 // Pipeline: the fragments of a stage's two k-steps are read half a stage ahead of their MFMAs; one barrier
 // per stage, in the middle of the MFMAs, frees the buffer just read for the stage S ahead.
+//
+// What bounds it, with the us of a whole call (the launches one by one on a stream): short buckets the
+// weights' way from memory, by which a call of 32 tokens (DeepSeek-V2-Lite sizes, 48 of 64 experts resident,
+// 408 MB of weights) takes 83 us, its up launch at 5.2 TB/s of the 6.25 that a plain read reaches; one token
+// (43 MB) the launches' starts and ends, 20 us; long buckets the matrix units (Qwen2 sizes, T = 4096, 3.6
+// TOP: 2120 us with up at 1.84 and down at 1.69 POP/s, where a plain int8 product of 8192^3 reaches 2.13).
+// In between (T = 1000, 157 us) neither: 2.75 rounds of blocks whose stages wait for weights and tokens alike.
+// Kernels that kept a few tokens' rows in registers and streamed the weights past them, rings of other depths
+// for weights and tokens, and loads issued by half of the waves were not faster for any T.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -604,7 +613,9 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2))
 
 // Rows of H to 8 bits: a block per kQuantRow values of a row, the T shared rows first, then the HIT slots'
 // positions.  The row's maximum comes from the partial maxima that the up tiles left, one per `group`
-// features, so a row's blocks need not wait for each other; the values are on their way meanwhile.
+// features, so a row's blocks need not wait for each other; the values are on their way meanwhile.  Bound by
+// memory: Qwen2 sizes, T = 4096, 671 MB read and 168 MB written in 147 us, 5.7 TB/s; a few rows take 3 us, a
+// launch's own time. 
 constexpr int kQuantThreads = 256;
 constexpr int kQuantVec = 4;  // 16-byte chunks per thread
 constexpr int kQuantRow = kQuantVec * 4 * kQuantThreads;

@@ -219,8 +219,8 @@ __device__ int wave_topk_gates(const RouteArgs& a, int t, const double* z, const
     if constexpr (kScored) {
         double g = lane < K ? z[my_e] : 0.0;
         const double sum = (a.norm_topk || a.conf_mode == SPICE_CONF_GATE_RENORM) ? route_wave_sum(g) : 1.0;
-        if (a.norm_topk) g = sum > 0.0 ? g / sum : 0.0;
-        const double gsum = a.norm_topk || !(sum > 0.0) ? 1.0 : sum;
+        if (a.norm_topk) g = sum == 0.0 ? 0.0 : g / sum;
+        const double gsum = a.norm_topk || sum == 0.0 ? 1.0 : sum;
         if (lane >= K) return -1;
         return slot_outputs<kPublish>(a, t, res, lane, my_e, g, gsum, (float)(g * (double)a.scale), conf_in);
     }
@@ -370,7 +370,7 @@ __device__ void block_topk_scored(const RouteArgs& a, int t, const double* zg, S
         __syncthreads();
         double sum = L.red[1][0];
         for (int i = 1; i < waves; ++i) sum += L.red[1][i];
-        s = s > 0.0 ? s / sum : 0.0;
+        s = s == 0.0 ? 0.0 : s / sum;
     }
     if (tid < N) {
         L.s[tid] = s;
@@ -419,7 +419,7 @@ __device__ inline void wave_topk_scored(const RouteArgs& a, double* z, double* c
         const double sum = route_wave_sum(part);
 #pragma unroll
         for (int j = 0; j < kJ; ++j)
-            if (64 * j < N) s[j] = s[j] > 0.0 ? s[j] / sum : 0.0;
+            if (64 * j < N) s[j] = s[j] == 0.0 ? 0.0 : s[j] / sum;
     }
 #pragma unroll
     for (int j = 0; j < kJ; ++j) {
