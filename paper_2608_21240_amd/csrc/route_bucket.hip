@@ -283,9 +283,9 @@ __global__ __launch_bounds__(kPrefillThreads) void route_tiled_kernel(RouteArgs 
         const int tt = w + h * kNW;
         const unsigned long long* kr = L.key[tt];
         if constexpr (kScored) {
-            // the partial logits are summed: their region holds the waves' group values
-            static_assert(sizeof(GroupLds) * kNW <= sizeof(L.zp), "group values fit the partial logits' region");
-            wave_topk_scored(a, L.z[tt], reinterpret_cast<double*>(L.key[tt]), reinterpret_cast<GroupLds*>(L.zp)[w],
+            // the partial logits are summed: their region holds the waves' scratch
+            static_assert(sizeof(WaveTopkLds) * kNW <= sizeof(L.zp), "the waves' scratch fits the partial logits' region");
+            wave_topk_scored(a, L.z[tt], reinterpret_cast<double*>(L.key[tt]), reinterpret_cast<WaveTopkLds*>(L.zp)[w],
                              L.pick[tt]);
             continue;
         }

@@ -392,9 +392,17 @@ __device__ void block_topk_scored(const RouteArgs& a, int t, const double* zg, S
     if (w == 0) wave_topk_gates<true, true>(a, t, L.s, L.res, L.pick, lane, conf_in);
 }
 
+// LDS of wave_topk_scored: the groups, then the candidates for the picks.
+struct WaveTopkLds {
+    GroupLds group;
+    double value[SPICE_MAX_EXPERTS];
+    int id[SPICE_MAX_EXPERTS];
+};
+
 // The same by one wave: z = the token's N logits in, its scores out; c = its choice values; pick = its K
-// experts (all in LDS).
-__device__ inline void wave_topk_scored(const RouteArgs& a, double* z, double* c, GroupLds& G, int* pick) {
+// experts (all in LDS).  Of more than 64 experts only those are ranked that reach the K-th largest of the
+// lanes' maxima, as K experts do: 64 compares per lane and a few more instead of N^2 / 64.
+__device__ inline void wave_topk_scored(const RouteArgs& a, double* z, double* c, WaveTopkLds& L, int* pick) {
     constexpr int kJ = SPICE_MAX_EXPERTS / 64;
     const int N = a.N, lane = threadIdx.x & 63;
     auto sync = [] {  // a wave's LDS accesses complete in order; only the compiler has to keep theirs
@@ -432,14 +440,55 @@ __device__ inline void wave_topk_scored(const RouteArgs& a, double* z, double* c
     }
     sync();
     if (a.n_group > 1) {
-        keep_groups(a, c, G, lane, 64, sync);
+        keep_groups(a, c, L.group, lane, 64, sync);
         sync();
     }
-    int r[kJ];
-    count_before(c, N, 0, N, lane, r);
+    if (N <= 64) {
+        int r[kJ];
+        count_before(c, N, 0, N, lane, r);
+        if (lane < N && r[0] < a.K) pick[r[0]] = lane;
+        return;
+    }
+    double top = kExcluded;
 #pragma unroll
-    for (int j = 0; j < kJ; ++j)
-        if (lane + 64 * j < N && r[j] < a.K) pick[r[j]] = lane + 64 * j;
+    for (int j = 0; j < kJ; ++j) {
+        v[j] = lane + 64 * j < N ? c[lane + 64 * j] : -INFINITY;
+        top = fmax(top, v[j]);
+    }
+    double* tops = L.group.value;
+    static_assert(kMaxGroups >= 64, "a value per lane");
+    tops[lane] = top;
+    sync();
+    int before = 0;
+#pragma unroll 8
+    for (int i = 0; i < 64; ++i) {
+        const double other = tops[i];
+        before += (int)((other > top) | ((other == top) & (i < lane)));
+    }
+    const double least = tops[__ffsll((long long)__ballot(before == a.K - 1)) - 1];
+    int n = 0;
+#pragma unroll
+    for (int j = 0; j < kJ; ++j) {
+        const bool cand = v[j] >= least;
+        const unsigned long long m = __ballot(cand);
+        if (cand) {
+            const int at = n + __popcll(m & (lane == 0 ? 0ull : ~0ull >> (64 - lane)));
+            L.value[at] = v[j];
+            L.id[at] = lane + 64 * j;
+        }
+        n += __popcll(m);
+    }
+    sync();
+    for (int i = lane; i < n; i += 64) {  // in id order, so of equal values the earlier one comes first
+        const double mine = L.value[i];
+        int r = 0;
+#pragma unroll 4
+        for (int k = 0; k < n; ++k) {
+            const double other = L.value[k];
+            r += (int)((other > mine) | ((other == mine) & (k < i)));
+        }
+        if (r < a.K) pick[r] = L.id[i];
+    }
 }
 
 // LDS of block_topk.
