@@ -20,12 +20,13 @@
 //   3. bucket_scatter_kernel: per 16 tokens, the stable positions of their slots (perm,
 //      inv_perm).  The last scan block also writes the host copies when asked.
 // By a scoring rule (moe_route_bucket_scored) few tokens take route_scored_kernel, the same steps in
-//   blocks of 8 waves, and more of them route_tiled_kernel<kScored>, whose waves rank a token each.  A token
-//   costs its logits, and its last block the ranks: N^2 compares of doubles in LDS, and the groups' before
-//   them.  us per call (sigmoid / softmax of 8 groups with a balance bias): N = 64, d = 2048, K = 6: T = 1
-//   9.2 / 10.9, T = 32 11.0 / 12.7, T = 1000 27 / 29; N = 256, d = 3584, K = 8: T = 48 26 / 28, T = 128 43 /
-//   46, T = 250 73 / 76; N = 64, d = 3584, T = 4096 52 / 55, of which the logits' 1.9 GFLOP in fp64 take 26
-//   at the card's 73 TFLOP/s.
+//   blocks of 8 waves, and more of them (scored_keeps_rows) route_tiled_kernel<kScored>, whose waves rank a
+//   token each.  Few tokens are bound by the way from a block's start through the logits, its token's last
+//   block and the last of all, more by the logits' fp64 products, each token with its own pass over the router
+//   in the row form.  us per call (sigmoid / softmax of 8 groups with a balance bias): N = 64, d = 2048, K = 6:
+//   T = 1 9.2 / 10.9, T = 32 11.0 / 12.7, T = 1000 27 / 29; N = 256, d = 3584, K = 8: T = 48 26 / 29, T = 96
+//   35 / 38, T = 250 46 / 50; N = 64, d = 3584, T = 4096 52 / 55, of which the logits' 1.9 GFLOP take 26 at the
+//   card's 73 TFLOP/s in fp64.
 // The tiled logits are bound by the fp64 matrix rate of the CUs that hold a block: with a block
 // per 16 tokens, 63 CUs at T = 1000; with the contraction split, all 256 (N = 64, d = 2048: the
 // three launches 40 -> 26 us).  Below kRouteTiledMinT the row-per-wave launch is shorter (rows /
@@ -500,7 +501,7 @@ template <int DT, bool kScored>
 hipError_t launch_route(const RouteArgs& a, hipStream_t s) {
     const unsigned groups = (unsigned)((a.T + kPrefillTok - 1) / kPrefillTok);
     const int parts = route_parts(a.T, a.N, a.d, a.dtype, a.part_bytes);
-    if (route_keeps_rows(a.T, a.N, a.d, parts, a.hx != nullptr)) {
+    if ((kScored ? scored_keeps_rows : route_keeps_rows)(a.T, a.N, a.d, parts, a.hx != nullptr)) {
         if constexpr (kScored) return launch_scored_rows<DT>(a, s);
         const int g = route_blocks_per_token(a.N + (a.w_sg ? 1 : 0), kLogitThreads);
         hipLaunchKernelGGL(route_logits_kernel<DT>, dim3((unsigned)(a.T * g)), dim3(kLogitThreads), 0, s, a, g);

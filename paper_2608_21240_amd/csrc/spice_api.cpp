@@ -183,7 +183,7 @@ WsLayout ws_layout(const spice_moe_cfg_t& c, int32_t T) {
     L.top_s = off;  off += i8 ? align256(t * (size_t)c.shared_inter / 16 * sizeof(float)) : 0;
     L.base = off;
     L.zpart = off;
-    if (T >= kRouteTiledMinT) {
+    if (T >= kRouteTiledMinT || (int64_t)T * c.n_experts >= kScoredTiledMinSlots) {
         const size_t groups = (t + kRouteTileTok - 1) / kRouteTileTok;
         const int zp = route_parts(T, c.n_experts, c.d, c.dtype, SIZE_MAX);
         if (zp > 1) off += align256((size_t)zp * groups * kRouteTileTok * c.n_experts * sizeof(double));

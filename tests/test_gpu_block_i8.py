@@ -226,9 +226,11 @@ def test_bad_logits_still_give_valid_experts(T):
         r.check_buckets()
 
 
-@pytest.mark.parametrize("T,N,K", [(13, 40, 5), (16, 40, 4), (64, 9, 1), (128, 256, 8), (207, 256, 2), (208, 16, 2)])
+@pytest.mark.parametrize("T,N,K", [(13, 40, 5), (16, 40, 4), (64, 9, 1), (109, 256, 8), (110, 256, 8), (207, 256, 2),
+                                   (208, 128, 2), (218, 128, 2), (219, 128, 64), (256, 109, 3), (256, 110, 3), (257, 16, 2)])
 def test_scored_routing_at_the_limits_of_its_variants(T, N, K):
-    """64 and 65 slots, 1, 2 and 4 rows per wave, the last and the first T of the row and tile forms."""
+    """64 and 65 slots, 1, 2 and 4 rows per wave, the last and the first calls of the row and tile forms, and of
+    the form with separate bucketing."""
     for rule in RULES:
         r = Routing(T, 128, N, K, C=N // 2, seed=T)
         if N % rule.get("groups", 1) or K > rule.get("keep", 1) * (N // rule.get("groups", 1)):
@@ -240,6 +242,21 @@ def test_scored_routing_at_the_limits_of_its_variants(T, N, K):
 def test_scored_routing_of_many_tokens():
     r = Routing(20000, 64, 16, 3, C=5, seed=3, norm_topk=1)
     rule = dict(sigmoid=True, groups=4, keep=2, top=2, balance=True, scale=2.5)
+    r.run(**rule)
+    r.check(r.logits.cpu().numpy(), **rule)
+
+
+@pytest.mark.parametrize("T", [120, 300])
+@pytest.mark.parametrize("N,K,groups,keep", [(65, 64, 13, 13), (250, 64, 50, 13), (256, 1, 2, 1), (192, 30, 1, 1)])
+def test_scored_routing_ranks_of_more_experts_than_lanes(T, N, K, groups, keep):
+    """Few distinct scores, masked experts, K up to 64 and groups that leave hardly more: many candidates and ties."""
+    rule = dict(sigmoid=True, groups=groups, keep=keep, balance=True)
+    r = Routing(T, 64, N, K, seed=N + K)
+    g = R.gen(3)
+    r.x = torch.randint(-1, 2, (T, 64), generator=g).to(BF).cuda()
+    r.wg = (torch.randint(-1, 2, (N, 64), generator=g).to(BF) / 8).cuda()
+    r.balance = torch.zeros_like(r.balance)
+    r.bias = torch.where(torch.rand(N, generator=g) < 0.3, -float("inf"), 0.0).cuda()
     r.run(**rule)
     r.check(r.logits.cpu().numpy(), **rule)
 
