@@ -44,33 +44,36 @@
 namespace spice {
 namespace {
 
-template <int BM_, int BT_, int WF_, int WT_, int S_, int L_>
+template <int BM_, int BT_, int WF_, int WT_, int S_, int SW_>
 struct Shape {
-    static constexpr int BM = BM_, BT = BT_, WF = WF_, WT = WT_, S = S_;
+    static constexpr int BM = BM_, BT = BT_, WF = WF_, WT = WT_;
+    static constexpr int S = S_, SW = SW_;         // stages of tokens and of weights in LDS
     static constexpr int kThreads = 64 * WF * WT;
-    static constexpr int kLoaders = 64 * L_;       // threads that issue the stages' loads
+    static constexpr int kLoaders = 256;           // threads that issue the stages' loads
     static constexpr int RF = BM / WF / 16;        // 16-row sub-tiles per wave
     static constexpr int RT = BT / WT / 16;        // 16-token sub-tiles per wave
     static constexpr int kTStride = 16 * WT;       // tile rows between a wave's token sub-tiles
     static constexpr int kUpFeat = BM / 2;         // features of an up tile (W1 rows = W3 rows)
     static constexpr int kTopGroup = kUpFeat / WF; // features of a wave: those of a partial maximum of H
     static constexpr int kWTile = BM * 128;        // bytes of a stage's weight rows
-    static constexpr int kStage = (BM + BT) * 128;
+    static constexpr int kXTile = BT * 128;        // and of its token rows
+    static constexpr int kLds = SW * kWTile + S * kXTile;
     static constexpr int kRowStep = kLoaders / 8;  // rows one load instruction of the loaders covers
     static constexpr int kWLoads = BM / kRowStep, kXLoads = BT / kRowStep;
-    static constexpr int kXcdBlocks = 32 * std::max(1, 163840 / (S * kStage));  // resident blocks per XCD
+    static constexpr int kXcdBlocks = 32 * std::max(1, 163840 / kLds);  // resident blocks per XCD
     static constexpr int kAccs = RF * RT * 4;      // sums per thread
     static_assert(kRowStep % 16 == 0 && kUpFeat % kRowStep == 0, "staged rows keep their swizzle");
     static_assert(BM % kRowStep == 0 && BT % kRowStep == 0, "whole load instructions");
-    static_assert((S - 1) * (kWLoads + kXLoads) < 64, "vmcnt holds the loads in flight");
+    static_assert(SW == S || SW == S + 1, "weights are at most a stage ahead of the tokens");
+    static_assert(S * (kWLoads + kXLoads) < 64, "vmcnt holds the loads in flight");
 };
 using Tile64x32 = Shape<64, 32, 2, 2, 4, 4>;
-using Tile128x64 = Shape<128, 64, 2, 2, 3, 4>;
-using Tile128x128 = Shape<128, 128, 2, 4, 2, 4>;
-using Tile256x256 = Shape<256, 256, 2, 4, 2, 4>;
+using Tile128x64 = Shape<128, 64, 2, 2, 3, 3>;
+using Tile128x128 = Shape<128, 128, 2, 4, 2, 3>;
+using Tile256x256 = Shape<256, 256, 2, 4, 2, 3>;
 template <class C>
 constexpr bool matches(const I8Shape& s) {
-    return C::BM == s.rows && C::BT == s.tokens && C::S * C::kStage == s.lds;
+    return C::BM == s.rows && C::BT == s.tokens && C::kLds == s.lds;
 }
 static_assert(matches<Tile64x32>(kI8Shapes[0]) && matches<Tile128x64>(kI8Shapes[1]) && matches<Tile128x128>(kI8Shapes[2]) &&
                   matches<Tile256x256>(kI8Shapes[3]),
@@ -295,17 +298,19 @@ template <class C, bool kUp, bool kBf16, int NL, class Load>
 __device__ __forceinline__ void product(unsigned char* s_lds, int nk, uint32_t fbase, uint32_t tbase, Load load,
                                         i32x4_t (&acc)[C::RF][C::RT]) {
     constexpr int N1 = NL > 0 ? NL : 1;
-    constexpr int kLoads = (C::S - 2) * (C::kWLoads + C::kXLoads);  // stages in flight past the next one
-    auto read = [&](int buf, uint32_t kx, Frags<C, N1>& f) {
+    // loads in flight past the next stage's: whole stages, and the last weights issued, which are a stage ahead
+    constexpr int kLoads = (C::S - 2) * (C::kWLoads + C::kXLoads) + (C::SW - C::S) * C::kWLoads;
+    auto read = [&](int wbuf, int xbuf, uint32_t kx, Frags<C, N1>& f) {
         if constexpr (NL > 0) {
-            const unsigned char* base = s_lds + buf * C::kStage;
+            const unsigned char* wbase = s_lds + wbuf * C::kWTile;
+            const unsigned char* xbase = s_lds + C::SW * C::kWTile + xbuf * C::kXTile;
 #pragma unroll
             for (int t = 0; t < NL; ++t)
-                f.b[t] = *reinterpret_cast<const i32x4_t*>(base + ((tbase + t * C::kTStride * 128) ^ kx));
+                f.b[t] = *reinterpret_cast<const i32x4_t*>(xbase + ((tbase + t * C::kTStride * 128) ^ kx));
 #pragma unroll
             for (int s = 0; s < C::RF; ++s) {
                 const int row = kUp ? (s % (C::RF / 2)) * 16 + (s / (C::RF / 2)) * C::kUpFeat : s * 16;
-                f.a[s] = *reinterpret_cast<const i32x4_t*>(base + ((fbase + row * 128) ^ kx));
+                f.a[s] = *reinterpret_cast<const i32x4_t*>(wbase + ((fbase + row * 128) ^ kx));
             }
         }
     };
@@ -329,18 +334,19 @@ __device__ __forceinline__ void product(unsigned char* s_lds, int nk, uint32_t f
     };
     wait_and_barrier<kLoads + C::kWLoads + C::kXLoads>();  // stage 0 of the S in flight has landed
     Frags<C, N1> f0, f1;
-    read(0, 0u, f0);
-    int buf = 0;
+    read(0, 0, 0u, f0);
+    int wbuf = 0, xbuf = 0;
     for (int kt = 0; kt < nk; ++kt) {
-        read(buf, 64u, f1);
+        read(wbuf, xbuf, 64u, f1);
         __builtin_amdgcn_sched_barrier(0);
         mma(f0);
         __builtin_amdgcn_sched_barrier(0);
         // stage kt + 1 has landed and every wave has read all of stage kt
         wait_and_barrier<kLoads>();
-        load(buf, kt + C::S);
-        buf = buf + 1 == C::S ? 0 : buf + 1;
-        read(buf, 0u, f0);  // past the last stage: zeros, unused
+        load(wbuf, xbuf, kt);
+        wbuf = wbuf + 1 == C::SW ? 0 : wbuf + 1;
+        xbuf = xbuf + 1 == C::S ? 0 : xbuf + 1;
+        read(wbuf, xbuf, 0u, f0);  // past the last stage: zeros, unused
         __builtin_amdgcn_sched_barrier(0);
         mma(f1);
         __builtin_amdgcn_sched_barrier(0);
@@ -392,7 +398,6 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2))
     extern __shared__ __align__(16) unsigned char s_lds[];
     const FfnI8Args& a = job.a;
     Tile j;
-    __shared__ int s_last;
     if (!resolve<kUp, C>(job, job.xcd ? xcd_tile(blockIdx.x, gridDim.x, C::kXcdBlocks) : (int)blockIdx.x, j)) return;
     if constexpr (!kUp) {
         if (j.lore) {
@@ -436,7 +441,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2))
     auto stage_k = [&](int kt) { return kt >= nk ? 0x800000 : j.k0 + (kt + rot >= nk ? kt + rot - nk : kt + rot); };
     auto load_w = [&](int buf, int kt) {
         if (!loader) return;
-        unsigned char* run = s_lds + buf * C::kStage + w * 1024;
+        unsigned char* run = s_lds + buf * C::kWTile + w * 1024;
         kt = stage_k(kt);
         const bool in = kt * kBK < klim;
 #pragma unroll
@@ -449,7 +454,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2))
     uint32_t xoff[C::kXLoads];
     auto load_x = [&](int buf, int kt) {
         if (!loader) return;
-        unsigned char* run = s_lds + buf * C::kStage + w * 1024 + C::kWTile;
+        unsigned char* run = s_lds + C::SW * C::kWTile + buf * C::kXTile + w * 1024;
         kt = stage_k(kt);
         const bool in = kt * kBK < klim;
 #pragma unroll
@@ -457,9 +462,10 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2))
             load_lds16(xbuf, in && xoff[i] != kOutOfRange ? xoff[i] + (uint32_t)kt * kBK : kOutOfRange,
                        run + i * C::kRowStep * 128);
     };
-    auto load = [&](int buf, int kt) {
-        load_w(buf, kt);
-        load_x(buf, kt);
+    // what takes the place of stage kt, the tokens first: a wait for them by count leaves the weights in flight
+    auto load = [&](int wbuf, int xbuf, int kt) {
+        load_x(xbuf, kt + C::S);
+        load_w(wbuf, kt + C::SW);
     };
     // the slot ids of the tile's rows, the weights of stage 0, then (once the ids are there) its token
     // rows and the other stages of the ring
@@ -516,12 +522,15 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2))
         for (int t = 0; t < C::RT; ++t) factor[t] = row_factor(rid[t]);
     }
 #pragma unroll
-    for (int s = 1; s < C::S; ++s) load(s, s);
+    for (int s = 1; s < C::SW; ++s) {
+        load_w(s, s);
+        if (s < C::S) load_x(s, s);
+    }
 
     // LDS addresses of the fragments of k-step 0 (k-step 1 reads chunk c ^ 4: bit 6 flipped).  The swizzle
     // of row r depends on (r >> 1) & 7, which steps of 16 rows leave unchanged.
     const uint32_t fbase = lds_off(frow0 + m, quad);
-    const uint32_t tbase = C::kWTile + lds_off(wt * 16 + m, quad);
+    const uint32_t tbase = lds_off(wt * 16 + m, quad);
     static_assert(C::RT == 1 || C::RT == 2 || C::RT == 4, "token sub-tiles per wave");
     auto multiply = [&](auto bf16) {
         constexpr bool kBf16 = decltype(bf16)::value;
@@ -558,7 +567,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2))
         if (j.split >= 0) {
             // the last of the tile's parts to arrive adds the others' sums to its own (exact: in any order)
             int32_t* part = a.part + (size_t)j.split * job.parts * C::kAccs * C::kThreads + tid;
-            if (!split_sums<C>(a, job.parts, j.split, j.part, part, acc, &s_last)) return;
+            if (!split_sums<C>(a, job.parts, j.split, j.part, part, acc, reinterpret_cast<int*>(s_lds))) return;
         }
     }
 
@@ -690,7 +699,7 @@ hipError_t launch_pass(const FfnI8Args& a, const I8Plan& plan, hipStream_t s) {
     if (tiles > 0x7FFFFFFFll) return hipErrorInvalidValue;
     job.lore = (int32_t)lore;
     if (a.Is > 0 && plan.xcd) super_shape((int)tiles_of(a.T, C::BT), (int)nt_sh, C::kXcdBlocks, job.super);
-    hipLaunchKernelGGL((i8_gemm_kernel<kUp, C>), dim3((unsigned)tiles), dim3(C::kThreads), C::S * C::kStage, s, job);
+    hipLaunchKernelGGL((i8_gemm_kernel<kUp, C>), dim3((unsigned)tiles), dim3(C::kThreads), C::kLds, s, job);
     return hipGetLastError();
 }
 

@@ -215,7 +215,7 @@ struct SpecArgs {
 struct I8Shape {
     int rows, tokens, lds;
 };
-constexpr I8Shape kI8Shapes[4] = {{64, 32, 49152}, {128, 64, 73728}, {128, 128, 65536}, {256, 256, 131072}};
+constexpr I8Shape kI8Shapes[4] = {{64, 32, 49152}, {128, 64, 73728}, {128, 128, 81920}, {256, 256, 163840}};
 
 // How a call of the 8-bit expert FFN runs.
 // shape: by the mean bucket n = T K / N, since a tile as tall as the buckets are long reads each weight
