@@ -22,14 +22,16 @@
 // XOR-swizzled by row (chunk c of row r at c ^ ((r >> 1) & 7)).  A chunk past the end of a row, and a row
 // past the end of a matrix or a bucket, reads zero (an offset past the buffer).
 // Pipeline: the fragments of a stage's two k-steps are read half a stage ahead of their MFMAs; one barrier
-// per stage, in the middle of the MFMAs, frees the buffer just read for the stage S ahead.
+// per stage, in the middle of the MFMAs, frees the buffer just read for the stage S ahead.  In the tall tiles
+// the weights' ring is a stage deeper than the tokens', which L2 holds (T = 4096 below 2117 -> 2022 us).
 //
 // What bounds it, with the us of a whole call (the launches one by one on a stream): short buckets the
 // weights' way from memory, by which a call of 32 tokens (DeepSeek-V2-Lite sizes, 48 of 64 experts resident,
 // 408 MB of weights) takes 83 us, its up launch at 5.2 TB/s of the 6.25 that a plain read reaches; one token
-// (43 MB) the launches' starts and ends, 20 us; long buckets the matrix units (Qwen2 sizes, T = 4096, 3.6
-// TOP: 2120 us with up at 1.84 and down at 1.69 POP/s, where a plain int8 product of 8192^3 reaches 2.13).
-// In between (T = 1000, 157 us) neither: 2.75 rounds of blocks whose stages wait for weights and tokens alike.
+// (43 MB) the launches' starts and ends, 19 us; long buckets the matrix units (Qwen2 sizes, T = 4096, 3.6
+// TOP: 2000 us with up at 1.96 and down at 1.80 POP/s, where a plain int8 product of 8192^3 reaches 2.13).
+// In between (T = 1000, 152 us) neither: 2.75 rounds of blocks, 115 us even where every expert has the same
+// weights, which L2 then holds.
 // Kernels that kept a few tokens' rows in registers and streamed the weights past them, rings of other depths
 // for weights and tokens, and loads issued by half of the waves were not faster for any T.
 #include <hip/hip_runtime.h>

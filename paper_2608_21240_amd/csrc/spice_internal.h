@@ -220,20 +220,20 @@ constexpr I8Shape kI8Shapes[4] = {{64, 32, 49152}, {128, 64, 73728}, {128, 128, 
 // How a call of the 8-bit expert FFN runs.
 // shape: by the mean bucket n = T K / N, since a tile as tall as the buckets are long reads each weight
 //   once; then smaller ones until the up launch fills the CUs, which takes more blocks the taller they are.
-//   us per call, shapes 0 .. 3: DeepSeek-V2-Lite sizes, 48 of 64 experts resident, T = 64 (n = 6) 90 / 95 /
-//   109 / 134, T = 130 (n = 12) 98 / 96 / 111 / 138, T = 219 (n = 20) 107 / 99 / 116 / 148, T = 500 (n = 46)
-//   152 / 121 / 127 / 157, T = 700 (n = 65) 180 / 146 / 136 / 164, T = 1000 (n = 93) 231 / 169 / 151 / 176,
-//   all resident T = 2000 (n = 187) 490 / 329 / 296 / 289; Qwen2 sizes T = 300 (n = 37) 617 / 481 / 499 /
-//   620, T = 500 (n = 62) 824 / 594 / 558 / 669, T = 1000 (n = 125) 1418 / 895 / 771 / 769.  Small layers
-//   (d, experts, their inter, shared inter; up blocks): 1024, 8, 512, 1024, T = 500 26 (1024) / 22 (256) / 26
-//   (128) / 51 (32); 1024, 4, 1024, 1024, T = 1000 49 / 37 (768) / 34 (384) / 58 (96).
+//   us per call, shapes 0 .. 3: DeepSeek-V2-Lite sizes, 48 of 64 experts resident, T = 64 (n = 6) 90 / 95,
+//   T = 130 (n = 12) 98 / 96, T = 219 (n = 20) 107 / 99 / 113 / 134, T = 400 (n = 37) 139 / 116 / 121 / 137,
+//   T = 700 (n = 65) 180 / 146 / 134 / 149, T = 1000 (n = 93) 231 / 169 / 150 / 163, all resident T = 1400
+//   (n = 131) 365 / 255 / 237 / 238, T = 2000 (n = 187) 490 / 329 / 293 / 278; Qwen2 sizes T = 300 (n = 37) 617 /
+//   481 / 470 / 560, T = 500 (n = 62) 824 / 594 / 530 / 600, T = 1000 (n = 125) 1418 / 895 / 738 / 709.  Small
+//   layers (d, experts, their inter, shared inter; up blocks): 1024, 8, 512, 1024, T = 500 26 (1024) / 22 (256)
+//   / 26 (128) / 51 (32); 1024, 4, 1024, 1024, T = 1000 49 / 37 (768) / 34 (384) / 58 (96).
 // parts: splits of the shared block's down contraction where its tiles would outlast the routed ones (Qwen2,
 //   T = 1 105 -> 88 us; T = 8, whose routed tiles take as long, 246 / 247), of 16 stages at least, as long
 //   as the GPU holds their blocks at once and their sums take 16 MiB at most.
 // xcd: whether an XCD's resident blocks take neighbouring tiles, a few weight tiles x a few token tiles,
 //   rather than the token tiles of single weight tiles: for the longest buckets only (no / yes:
-//   DeepSeek-V2-Lite T = 4096 (n = 384) 486 / 492, T = 8192 (n = 768) 917 / 892, Qwen2 T = 1000 769 / 872,
-//   T = 4096 (n = 512) 2127 / 2120).
+//   DeepSeek-V2-Lite T = 4096 (n = 384) 474 / 483, T = 8192 (n = 768) 892 / 870, Qwen2 T = 1000 709 / 796,
+//   T = 4096 (n = 512) 2018 / 1981).
 struct I8Plan {
     int shape, parts, xcd;
 };
@@ -244,7 +244,7 @@ static_assert((kWordI8Parts + kI8PartTiles) * 4 <= SPICE_WS_CONTROL_BYTES, "cont
 inline I8Plan i8_plan(int32_t T, int32_t d, int32_t N, int32_t K, int32_t C, int32_t I, int32_t Is) {
     const int64_t n = (int64_t)T * K / (N > 0 ? N : 1), buckets = N < C ? N : C;
     I8Plan p{};
-    p.shape = n < 12 ? 0 : n < 52 ? 1 : n < 140 ? 2 : 3;
+    p.shape = n < 12 ? 0 : n < 48 ? 1 : n < 110 ? 2 : 3;
     for (; p.shape > 0; --p.shape) {
         const int64_t feat = kI8Shapes[p.shape].rows / 2, tok = kI8Shapes[p.shape].tokens;
         const int64_t up = ((T + tok - 1) / tok) * ((Is + feat - 1) / feat) + buckets * ((n + tok - 1) / tok) * ((I + feat - 1) / feat);

@@ -221,7 +221,7 @@ def of(layer, T, C):
 
 @pytest.mark.parametrize("layer,T,C,shape", [
     (DSV2, 1, 32, 0), (DSV2, 64, 48, 0), (DSV2, 219, 48, 1), (DSV2, 500, 48, 1), (DSV2, 700, 48, 2), (DSV2, 1000, 48, 2),
-    (DSV2, 2000, 64, 3), (QWEN2, 16, 64, 0), (QWEN2, 300, 64, 1), (QWEN2, 500, 64, 2), (QWEN2, 4096, 64, 3),
+    (DSV2, 2000, 64, 3), (QWEN2, 1000, 64, 3), (QWEN2, 16, 64, 0), (QWEN2, 300, 64, 1), (QWEN2, 500, 64, 2), (QWEN2, 4096, 64, 3),
     ((1024, 8, 2, 512, 1024), 500, 8, 1), ((1024, 4, 2, 1024, 1024), 1000, 4, 2), ((2048, 8, 2, 1024, 256), 700, 8, 1)])
 def test_tile_shapes(plan, layer, T, C, shape):
     assert plan(of(layer, T, C))[0][0] == shape
