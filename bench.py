@@ -58,8 +58,8 @@ TRAFFIC_RECORDS = {
                            "paper_2608_21240_amd/csrc/tile_index.h",
                            "paper_2608_21240_amd/csrc/combine.hip",
                            "paper_2608_21240_amd/csrc/spice_internal.h"),
-        "source_sha256_16": "9a7b80bd3eb358f0",
-        "fetch_kib_per_call": 12028.7 + 184115.6 + 90280.8 + 905.6,
+        "source_sha256_16": "048f74898073df35",
+        "fetch_kib_per_call": 12028.4 + 184119.7 + 90271.8 + 905.6,
         "write_kib_per_call": 260.2 + 675.8 + 1195.7 + 128.0,
         "fetch_factor": 2.0,
         "write_factor": 1.0,
@@ -75,9 +75,9 @@ TRAFFIC_RECORDS = {
                            "paper_2608_21240_amd/csrc/tile_index.h",
                            "paper_2608_21240_amd/csrc/combine.hip",
                            "paper_2608_21240_amd/csrc/spice_internal.h"),
-        "source_sha256_16": "9a7b80bd3eb358f0",
-        "fetch_kib_per_call": 12031.6 + 55308.9 + 26267.6 + 903.1,
-        "write_kib_per_call": 260.1 + 675.9 + 1195.9 + 128.0,
+        "source_sha256_16": "048f74898073df35",
+        "fetch_kib_per_call": 12021.2 + 55303.3 + 26299.3 + 903.1,
+        "write_kib_per_call": 260.1 + 675.8 + 1195.9 + 128.0,
         "fetch_factor": 2.0,
         "write_factor": 1.0,
         "profile": "profiles/ffn_dsv2_decode_T32_mxfp4.md",
@@ -88,8 +88,8 @@ TRAFFIC_RECORDS = {
                            "paper_2608_21240_amd/csrc/expert_ffn_tiles.h",
                            "paper_2608_21240_amd/csrc/tile_index.h",
                            "paper_2608_21240_amd/csrc/spice_internal.h"),
-        "source_sha256_16": "c8d0184604122224",
-        "fetch_kib_per_call": 189111.8 + 96776.7,
+        "source_sha256_16": "6ea4b5a97bbea81a",
+        "fetch_kib_per_call": 189113.8 + 96785.9,
         "write_kib_per_call": 462.4 + 1452.0,
         "fetch_factor": 2.0,
         "write_factor": 1.0,
@@ -102,8 +102,8 @@ TRAFFIC_RECORDS = {
                            "paper_2608_21240_amd/csrc/expert_ffn_tiles.h",
                            "paper_2608_21240_amd/csrc/tile_index.h",
                            "paper_2608_21240_amd/csrc/spice_internal.h"),
-        "source_sha256_16": "9f92c88ba9b965c5",
-        "fetch_kib_per_call": 60284.4 + 32795.2,
+        "source_sha256_16": "885a4525ab92c304",
+        "fetch_kib_per_call": 60286.4 + 32785.0,
         "write_kib_per_call": 462.6 + 1452.0,
         "fetch_factor": 2.0,
         "write_factor": 1.0,

@@ -27,13 +27,13 @@
 //
 // What bounds it, with the us of a whole call (the launches one by one on a stream): short buckets the
 // weights' way from memory, by which a call of 32 tokens (DeepSeek-V2-Lite sizes, 48 of 64 experts resident,
-// 408 MB of weights) takes 83 us, its up launch at 5.2 TB/s of the 6.25 that a plain read reaches; one token
+// about 410 MB of weights) takes 83 us, its up launch at 5.4 TB/s of the 6.25 that a plain read reaches; one token
 // (43 MB) the launches' starts and ends, 19 us; long buckets the matrix units (Qwen2 sizes, T = 4096, 3.6
 // TOP: 2000 us with up at 1.96 and down at 1.80 POP/s, where a plain int8 product of 8192^3 reaches 2.13).
 // In between (T = 1000, 152 us) neither: 2.75 rounds of blocks, 115 us even where every expert has the same
 // weights, which L2 then holds.
-// Kernels that kept a few tokens' rows in registers and streamed the weights past them, rings of other depths
-// for weights and tokens, and loads issued by half of the waves were not faster for any T.
+// Kernels that kept a few tokens' rows in registers and streamed the weights past them, and weights and tokens
+// loaded by different waves, were not faster for any T.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
