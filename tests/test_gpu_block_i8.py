@@ -429,6 +429,22 @@ def test_split_experts_in_a_graph_beside_an_eager_call():
             assert torch.equal(e.y_slots, w[0]) and torch.equal(e.y_shared, w[1])
 
 
+@pytest.mark.parametrize("T,K,I,Is", [(1, 6, 256, 512), (2, 4, 1408, 2816), (3, 4, 1408, 2816), (16, 1, 272, 1040),
+                                      (16, 2, 272, 0), (17, 2, 272, 16), (1, 8, 2576, 20480), (2, 1, 16, 10752),
+                                      (2, 1, 16, 10880)])
+@pytest.mark.parametrize("one", [False, True])
+def test_experts_of_few_rows(T, K, I, Is, one):
+    """Around the limits of down tiles that make H's codes for themselves; one: every slot takes the same expert,
+    a bucket of more entries than tokens."""
+    e = Experts(T, 64, 9, K, I, Is, 9, seed=T + K)
+    if one:
+        e.idx = torch.full((T, K), 3)
+        perm, inv, off = R.buckets_ref(e.idx.numpy(), e.cls.numpy(), 9)
+        e.perm, e.offsets, e.pos = torch.from_numpy(perm).int().cuda(), torch.from_numpy(off).int().cuda(), torch.from_numpy(inv).cuda()
+    e.run()
+    e.check()
+
+
 @pytest.mark.parametrize("T", [1, 20, 150, 400])
 def test_experts_with_gate_and_surrogates(T):
     e = Experts(T, 256, 8, 3, 96, 160, 4, r=16, seed=T, lore=True)
