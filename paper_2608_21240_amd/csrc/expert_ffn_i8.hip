@@ -28,7 +28,7 @@
 // What bounds it, with the us of a whole call (the launches one by one on a stream): short buckets the
 // weights' way from memory, by which a call of 32 tokens (DeepSeek-V2-Lite sizes, 48 of 64 experts resident,
 // about 410 MB of weights) takes 83 us, its up launch at 5.4 TB/s of the 6.25 that a plain read reaches; one token
-// (43 MB) the launches' starts and ends, 19 us; long buckets the matrix units (Qwen2 sizes, T = 4096, 3.6
+// (43 MB) the launches' starts and ends, 17 us; long buckets the matrix units (Qwen2 sizes, T = 4096, 3.6
 // TOP: 2000 us with up at 1.96 and down at 1.80 POP/s, where a plain int8 product of 8192^3 reaches 2.13).
 // In between (T = 1000, 152 us) neither: 2.75 rounds of blocks, 115 us even where every expert has the same
 // weights, which L2 then holds.
@@ -527,15 +527,17 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2))
 #pragma unroll
         for (int t = 0; t < C::RT; ++t) rid[t] = row_id(t);
     }
-    // kOwn: wave w makes the codes of the rows w, w + 4, .. as the quantisation launch does; the first row's
-    // values come before the ring's first loads
+    // kOwn: the waves make the codes of the rows as the quantisation launch does, a wave each, or a half or a
+    // quarter of one or two rows; the first values come before the ring's first loads
     const int own_rows = kOwn ? min(min(j.ntok - j.tok0, C::BT), job.own_rows) : 0, nv = j.kdim / 4;
-    const int v0 = j.k0 * (kBK / 4), v1 = min(j.k1 * (kBK / 4), nv), own_ld = nk_pad(j.kdim) + 16;
+    const int own_ld = nk_pad(j.kdim) + 16, segs = own_rows == 1 ? 4 : own_rows == 2 ? 2 : 1;
+    const int v_all = j.k0 * (kBK / 4), v_end = min(j.k1 * (kBK / 4), nv), seg_len = (v_end - v_all + segs - 1) / segs;
     float* s_top = reinterpret_cast<float*>(s_lds + C::SW * C::kWTile);
     constexpr int kOwnVec = 6;
     f32x4_t hv[kOwnVec];
     float hp = 0.f;
-    auto own_load = [&](int row) {
+    auto own_load = [&](int it) {
+        const int row = it / segs, v0 = v_all + it % segs * seg_len;
         const float* part = (j.shared ? a.top_s : a.top) + (row_first + row) * (j.kdim / 16);
         const int np = (j.kdim + job.group - 1) / job.group;
         hp = 0.f;
@@ -544,7 +546,8 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2))
 #pragma unroll
         for (int c = 0; c < kOwnVec; ++c) hv[c] = hr[min(v0 + lane + 64 * c, nv - 1)];
     };
-    auto own_store = [&](int row) {
+    auto own_store = [&](int it) {
+        const int row = it / segs, v0 = v_all + it % segs * seg_len, v1 = min(v0 + seg_len, v_end);
         float top = hp;
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) top = max_or_nan(top, __shfl_xor(top, o));
@@ -560,7 +563,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2))
         for (int i = v0 + lane + 64 * kOwnVec; i < v1; i += 64) codes[i] = pack_codes(hr[i], inv);
     };
     if constexpr (kOwn) {
-        if (w < own_rows) own_load(w);
+        if (w < own_rows * segs) own_load(w);
     }
     __builtin_amdgcn_sched_barrier(0);
     load_w(0, 0);
@@ -583,9 +586,9 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2))
     }
 
     if constexpr (kOwn) {
-        for (int row = w; row < own_rows; row += C::kThreads / 64) {
-            if (row != w) own_load(row);
-            own_store(row);
+        for (int it = w; it < own_rows * segs; it += C::kThreads / 64) {
+            if (it != w) own_load(it);
+            own_store(it);
         }
     }
     const uint32_t own_row = C::SW * C::kWTile + kOwnTops + (m < own_rows ? m : 0) * own_ld + quad * 16;
@@ -779,9 +782,9 @@ hipError_t launch_quant(const FfnI8Args& a, int group, hipStream_t s) {
 
 // A few short rows need no launch of their own: each down tile makes their codes for itself, while its
 // weights are on their way.  us per call with the launch / without: d = 512, 16 experts of 256, shared 512,
-// T = 1 14.3 / 11.5, T = 8 14.3 / 11.8; DeepSeek-V2-Lite sizes T = 1 22.5 / 21.2, T = 2 26.0 / 24.8.  Bytes of the
-// rows that a block holds at most, or 0 where three blocks of a CU have no room for them (with two, T = 4
-// 37.5 / 36.5, T = 12 66.0 / 68.7) or the tokens do not fit the tile.
+// T = 1 14.3 / 10.1, T = 8 14.3 / 11.2; DeepSeek-V2-Lite sizes T = 1 22.5 / 20.2, T = 2 26.0 / 23.2; Qwen2 sizes
+// T = 1 86.4 / 83.9.  Bytes of the rows that a block holds at most, or 0 where three blocks of a CU have no
+// room for them (with two, T = 4 37.4 / 36.5, T = 12 65.6 / 68.1) or the tokens do not fit the tile.
 int own_bytes(const FfnI8Args& a) {
     const long long rows = std::min<long long>((long long)a.T * a.K, OwnTile::BT);
     const long long bytes = std::max(a.Is > 0 ? (long long)a.T * (nk_pad(a.Is) + 16) : 0, rows * (nk_pad(a.I) + 16));
