@@ -58,8 +58,8 @@ TRAFFIC_RECORDS = {
                            "paper_2608_21240_amd/csrc/tile_index.h",
                            "paper_2608_21240_amd/csrc/combine.hip",
                            "paper_2608_21240_amd/csrc/spice_internal.h"),
-        "source_sha256_16": "048f74898073df35",
-        "fetch_kib_per_call": 12028.4 + 184119.7 + 90271.8 + 905.6,
+        "source_sha256_16": "1bcd0063098c4d68",
+        "fetch_kib_per_call": 12028.2 + 184121.3 + 90272.0 + 905.6,
         "write_kib_per_call": 260.2 + 675.8 + 1195.7 + 128.0,
         "fetch_factor": 2.0,
         "write_factor": 1.0,
@@ -75,9 +75,9 @@ TRAFFIC_RECORDS = {
                            "paper_2608_21240_amd/csrc/tile_index.h",
                            "paper_2608_21240_amd/csrc/combine.hip",
                            "paper_2608_21240_amd/csrc/spice_internal.h"),
-        "source_sha256_16": "048f74898073df35",
-        "fetch_kib_per_call": 12021.2 + 55303.3 + 26299.3 + 903.1,
-        "write_kib_per_call": 260.1 + 675.8 + 1195.9 + 128.0,
+        "source_sha256_16": "1bcd0063098c4d68",
+        "fetch_kib_per_call": 12020.6 + 55303.7 + 26301.8 + 903.1,
+        "write_kib_per_call": 260.0 + 675.8 + 1195.9 + 128.0,
         "fetch_factor": 2.0,
         "write_factor": 1.0,
         "profile": "profiles/ffn_dsv2_decode_T32_mxfp4.md",
@@ -88,8 +88,8 @@ TRAFFIC_RECORDS = {
                            "paper_2608_21240_amd/csrc/expert_ffn_tiles.h",
                            "paper_2608_21240_amd/csrc/tile_index.h",
                            "paper_2608_21240_amd/csrc/spice_internal.h"),
-        "source_sha256_16": "6ea4b5a97bbea81a",
-        "fetch_kib_per_call": 189113.8 + 96785.9,
+        "source_sha256_16": "acdfee8cac4f802c",
+        "fetch_kib_per_call": 189111.6 + 96772.1,
         "write_kib_per_call": 462.4 + 1452.0,
         "fetch_factor": 2.0,
         "write_factor": 1.0,
@@ -102,8 +102,8 @@ TRAFFIC_RECORDS = {
                            "paper_2608_21240_amd/csrc/expert_ffn_tiles.h",
                            "paper_2608_21240_amd/csrc/tile_index.h",
                            "paper_2608_21240_amd/csrc/spice_internal.h"),
-        "source_sha256_16": "885a4525ab92c304",
-        "fetch_kib_per_call": 60286.4 + 32785.0,
+        "source_sha256_16": "509691984fdb0f6c",
+        "fetch_kib_per_call": 60290.1 + 32779.9,
         "write_kib_per_call": 462.6 + 1452.0,
         "fetch_factor": 2.0,
         "write_factor": 1.0,

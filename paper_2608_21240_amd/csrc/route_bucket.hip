@@ -25,7 +25,7 @@
 //   block and the last of all, more by the logits' fp64 products, each token with its own pass over the router
 //   in the row form.  us per call (sigmoid / softmax of 8 groups with a balance bias): N = 64, d = 2048, K = 6:
 //   T = 1 9.2 / 10.9, T = 32 11.0 / 12.7, T = 1000 27 / 29; N = 256, d = 3584, K = 8: T = 48 26 / 29, T = 96
-//   35 / 38, T = 250 46 / 50; N = 64, d = 3584, T = 4096 52 / 55, of which the logits' 1.9 GFLOP take 26 at the
+//   30 / 34, T = 250 35 / 39; N = 64, d = 3584, T = 4096 52 / 55, of which the logits' 1.9 GFLOP take 26 at the
 //   card's 73 TFLOP/s in fp64.
 // The tiled logits are bound by the fp64 matrix rate of the CUs that hold a block: with a block
 // per 16 tokens, 63 CUs at T = 1000; with the contraction split, all 256 (N = 64, d = 2048: the
@@ -194,16 +194,21 @@ __device__ __forceinline__ void prefill_group(const RouteArgs& a, const char* xr
 constexpr int kTiledCache = 2048;  // slots whose keys stay in LDS while the last block buckets them
 constexpr size_t kTiledBucketLds = bucket_lds_bytes(kPrefillThreads, SPICE_MAX_EXPERTS, kTiledCache);
 
-// Tiled routing of the 16 tokens of group b / parts: the logits (part b % parts of the
+// Tiled routing of the 16 tokens of group b / blocks: the logits (part b % parts of the
 // contraction; the last of the group's blocks adds the parts in order), top-K, gates, classes.
 // kOne: the last block over all groups then buckets the slots (few tokens); otherwise the
-// group's histogram of bucket keys goes to column b / parts of the table.
+// group's histogram of bucket keys goes to column b / blocks of the table.
+// kScored: a group's blocks also share the experts, `chunk` each (whole groups of expert tiles), 64 or more,
+// which leaves fewer partial logits for its last block to add and busies more CUs (one chunk / this, us per
+// call: N = 256, d = 3584, T = 120 43 / 30, T = 250 46 / 35, T = 500 51 / 47; N = 128 the same).
+constexpr int kChunkExperts = 64;
 template <int DT, bool kOne, bool kScored>
-__global__ __launch_bounds__(kPrefillThreads) void route_tiled_kernel(RouteArgs a, int parts_k) {
+__global__ __launch_bounds__(kPrefillThreads) void route_tiled_kernel(RouteArgs a, int parts_k, int chunks_n, int chunk) {
     __shared__ __align__(16) unsigned char s_raw[sizeof(PrefillLds) > kTiledBucketLds ? sizeof(PrefillLds) : kTiledBucketLds];
     __shared__ int s_flag;
     PrefillLds& L = *reinterpret_cast<PrefillLds*>(s_raw);
-    const int group = blockIdx.x / parts_k, part_k = blockIdx.x % parts_k;
+    const int chunks = kScored ? chunks_n : 1, blocks = parts_k * chunks;  // of the group
+    const int group = blockIdx.x / blocks, part_k = blockIdx.x % parts_k;
     constexpr int kNW = kPrefillThreads / 64;
     const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, q = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -219,14 +224,16 @@ __global__ __launch_bounds__(kPrefillThreads) void route_tiled_kernel(RouteArgs 
     // logits: the expert tiles in groups of kGroupTiles; wave w takes group w / parts and
     // contraction part w % parts (parts = waves / groups), leaving its partial logits in LDS;
     // then the parts are summed in order
-    const int ntile = (N + 15) / 16, ngroups = (ntile + kGroupTiles - 1) / kGroupTiles, parts = kNW / ngroups;
+    const int e0 = kScored ? (int)blockIdx.x % blocks / parts_k * chunk : 0;  // and this block's experts
+    const int Nc = kScored ? min(chunk, N - e0) : N;
+    const int ntile = (Nc + 15) / 16, ngroups = (ntile + kGroupTiles - 1) / kGroupTiles, parts = kNW / ngroups;
     const int npass = (a.d + 8 * RouteElem<DT>::V - 1) / (8 * RouteElem<DT>::V);
     const int pa = part_k * npass / parts_k, np = (part_k + 1) * npass / parts_k - pa;  // this block's passes
     if (w < ngroups * parts) {
         const int g = w / parts, kp = w - g * parts;
         const int ntg = min(kGroupTiles, ntile - kGroupTiles * g);
         f64x4_t part[kGroupTiles];
-        prefill_group<DT>(a, xr, kGroupTiles * g, ntg, pa + kp * np / parts, pa + (kp + 1) * np / parts, lane, part);
+        prefill_group<DT>(a, xr, e0 / 16 + kGroupTiles * g, ntg, pa + kp * np / parts, pa + (kp + 1) * np / parts, lane, part);
         // result layout of the f64 16x16x4 product: element v of lane (m, q) is expert
         // tile*16 + 4v + q for token t0 + m
 #pragma unroll
@@ -234,16 +241,17 @@ __global__ __launch_bounds__(kPrefillThreads) void route_tiled_kernel(RouteArgs 
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
                 const int ee = (kGroupTiles * g + i) * 16 + 4 * v + q;
-                if (i < ntg && ee < N) L.zp[(kp * kPrefillTok + m) * N + ee] = part[i][v];
+                if (i < ntg && ee < Nc) L.zp[(kp * kPrefillTok + m) * Nc + ee] = part[i][v];
             }
     }
     __syncthreads();
-    for (int i = tid; i < kPrefillTok * N; i += kPrefillThreads) {
-        const int tt = i / N, ee = i - tt * N;
-        double z = L.zp[tt * N + ee];
-        for (int kp = 1; kp < parts; ++kp) z += L.zp[(kp * kPrefillTok + tt) * N + ee];
-        if (parts_k > 1) {  // written through to the device-coherent level (route_last_block)
-            __hip_atomic_store(reinterpret_cast<unsigned long long*>(a.part_ws) + (size_t)blockIdx.x * kPrefillTok * N + i,
+    for (int i = tid; i < kPrefillTok * Nc; i += kPrefillThreads) {
+        const int tt = i / Nc, ee = i - tt * Nc;
+        double z = L.zp[tt * Nc + ee];
+        for (int kp = 1; kp < parts; ++kp) z += L.zp[(kp * kPrefillTok + tt) * Nc + ee];
+        if (blocks > 1) {  // written through to the device-coherent level (route_last_block)
+            __hip_atomic_store(reinterpret_cast<unsigned long long*>(a.part_ws) +
+                                   ((size_t)(group * parts_k + part_k) * kPrefillTok + tt) * N + e0 + ee,
                                (unsigned long long)__double_as_longlong(z), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             continue;
         }
@@ -252,8 +260,8 @@ __global__ __launch_bounds__(kPrefillThreads) void route_tiled_kernel(RouteArgs 
         L.key[tt][ee] = logit_key(z);
         if (a.logits_out && t0 + tt < a.T) a.logits_out[(size_t)(t0 + tt) * N + ee] = z;
     }
-    if (parts_k > 1) {
-        if (!route_last_block(&a.ctrl[kWordTokCount + group * kTokCountStride], parts_k, &s_flag)) return;
+    if (blocks > 1) {
+        if (!route_last_block(&a.ctrl[kWordTokCount + group * kTokCountStride], blocks, &s_flag)) return;
         const unsigned long long* zp =
             reinterpret_cast<const unsigned long long*>(a.part_ws) + (size_t)group * parts_k * kPrefillTok * N;
         for (int i = tid; i < kPrefillTok * N; i += kPrefillThreads) {
@@ -319,7 +327,7 @@ __global__ __launch_bounds__(kPrefillThreads) void route_tiled_kernel(RouteArgs 
     if constexpr (kOne) {
         // the published top-K outputs and keys of every token are at the device-coherent level
         // once every group's last block has counted itself here
-        if (!route_last_block(&a.ctrl[kWordRouteDone], gridDim.x / parts_k, &s_flag)) return;
+        if (!route_last_block(&a.ctrl[kWordRouteDone], gridDim.x / blocks, &s_flag)) return;
         bucket_slots<kPrefillThreads, kTiledCache, true>(a, reinterpret_cast<int*>(s_raw));
         if (a.hx || a.h_idx || a.h_w || a.h_cls || a.h_ready) mirror_host<kPrefillThreads, true>(a);
         return;
@@ -500,19 +508,32 @@ hipError_t launch_scored_rows(const RouteArgs& a, hipStream_t s) {
 template <int DT, bool kScored>
 hipError_t launch_route(const RouteArgs& a, hipStream_t s) {
     const unsigned groups = (unsigned)((a.T + kPrefillTok - 1) / kPrefillTok);
-    const int parts = route_parts(a.T, a.N, a.d, a.dtype, a.part_bytes);
+    int parts = route_parts(a.T, a.N, a.d, a.dtype, a.part_bytes);
     if ((kScored ? scored_keeps_rows : route_keeps_rows)(a.T, a.N, a.d, parts, a.hx != nullptr)) {
         if constexpr (kScored) return launch_scored_rows<DT>(a, s);
         const int g = route_blocks_per_token(a.N + (a.w_sg ? 1 : 0), kLogitThreads);
         hipLaunchKernelGGL(route_logits_kernel<DT>, dim3((unsigned)(a.T * g)), dim3(kLogitThreads), 0, s, a, g);
         return hipGetLastError();
     }
-    const dim3 grid(groups * (unsigned)parts);
+    int chunks = 1, chunk = a.N;
+    if (kScored && parts > 1) {  // a block per CU at most, experts before parts of the contraction
+        const int per_group = (int)(256 / groups);  // at least parts
+        constexpr int kAlign = 16 * kGroupTiles;
+        const int want = a.N / kChunkExperts;
+        const int wide = want > 1 ? ((a.N + want - 1) / want + kAlign - 1) / kAlign * kAlign : a.N;
+        // where they come out uneven, the widest takes longer than the parts saved (N = 130, T = 1000 37 / 40 us)
+        if (want > 1 && want <= per_group && 4 * want * wide <= 5 * a.N) {
+            chunk = wide;
+            chunks = (a.N + wide - 1) / wide;
+            parts = std::max(1, std::min(parts, per_group / chunks));
+        }
+    }
+    const dim3 grid(groups * (unsigned)(parts * chunks));
     if (a.T <= kRouteTokenMaxT) {
-        hipLaunchKernelGGL((route_tiled_kernel<DT, true, kScored>), grid, dim3(kPrefillThreads), 0, s, a, parts);
+        hipLaunchKernelGGL((route_tiled_kernel<DT, true, kScored>), grid, dim3(kPrefillThreads), 0, s, a, parts, chunks, chunk);
         return hipGetLastError();
     }
-    hipLaunchKernelGGL((route_tiled_kernel<DT, false, kScored>), grid, dim3(kPrefillThreads), 0, s, a, parts);
+    hipLaunchKernelGGL((route_tiled_kernel<DT, false, kScored>), grid, dim3(kPrefillThreads), 0, s, a, parts, chunks, chunk);
     hipLaunchKernelGGL(bucket_scan_kernel, dim3((unsigned)((3 * a.N + kScanKeys - 1) / kScanKeys)), dim3(kScanThreads), 0, s,
                        a);
     hipLaunchKernelGGL(bucket_scatter_kernel, dim3(groups), dim3(64), 0, s, a);

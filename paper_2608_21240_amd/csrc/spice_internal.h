@@ -57,12 +57,12 @@ inline bool route_keeps_rows(int32_t T, int32_t N, int32_t d, int parts, bool x_
     if (T > kRouteTokenMaxT) return false;
     return x_to_host ? N >= 128 && d > 16 * T * parts : N < 56 || d > 4 * T * parts;
 }
-// The same for a scoring rule, whose tiles rank a token by one wave with few compares, and whose rows take 8
-// waves per block: by the ranks' and logits' number T N.  Rows / tiles, us per call: N = 256, d = 2048, T = 96
-// (25 k) 27.7 / 34.2, T = 128 (33 k) 31.9 / 34.6, T = 160 (41 k) 42.2 / 35.6, T = 250 58 / 38; N = 256, d = 512,
-// T = 96 27.6 / 27.4, T = 128 32.3 / 27.3; N = 128, d = 4096, T = 160 (20 k) 29.1 / 30.4, T = 207 (26 k) 34.9 /
-// 30.8; N = 64, d = 2048, T = 250 (16 k) 19.1 / 23.2.
-constexpr int kScoredTiledMinSlots = 28000;
+// The same for a scoring rule, whose tiles rank a token by one wave with few compares and share many experts
+// between blocks, and whose rows take 8 waves per block: by the ranks' and logits' number T N.  Rows / tiles, us
+// per call: N = 256, d = 3584, T = 64 (16 k) 26.4 / 29.7, T = 96 (25 k) 35.8 / 30.0, T = 207 61 / 34; d = 2048,
+// T = 96 28.2 / 29.7, T = 128 32.0 / 30.2; N = 128, d = 2048, T = 160 (20 k) 24.1 / 26.1, T = 207 (26 k) 26.8 /
+// 26.4; d = 4096, T = 160 29.1 / 26.6; N = 64, d = 2048, T = 250 (16 k) 19.1 / 23.2.
+constexpr int kScoredTiledMinSlots = 24000;
 inline bool scored_keeps_rows(int32_t T, int32_t N, int32_t d, int parts, bool x_to_host) {
     if (T > kRouteTokenMaxT || (int64_t)T * N >= kScoredTiledMinSlots) return false;
     return !x_to_host || route_keeps_rows(T, N, d, parts, x_to_host);

@@ -226,8 +226,8 @@ def test_bad_logits_still_give_valid_experts(T):
         r.check_buckets()
 
 
-@pytest.mark.parametrize("T,N,K", [(13, 40, 5), (16, 40, 4), (64, 9, 1), (109, 256, 8), (110, 256, 8), (207, 256, 2),
-                                   (208, 128, 2), (218, 128, 2), (219, 128, 64), (256, 109, 3), (256, 110, 3), (257, 16, 2)])
+@pytest.mark.parametrize("T,N,K", [(13, 40, 5), (16, 40, 4), (64, 9, 1), (93, 256, 8), (94, 256, 8), (207, 256, 2),
+                                   (187, 128, 2), (188, 128, 64), (300, 191, 3), (300, 130, 3), (256, 93, 3), (256, 94, 3), (257, 16, 2)])
 def test_scored_routing_at_the_limits_of_its_variants(T, N, K):
     """64 and 65 slots, 1, 2 and 4 rows per wave, the last and the first calls of the row and tile forms, and of
     the form with separate bucketing."""
