@@ -297,7 +297,7 @@ spice_status_t moe_expert_ffn_grouped_gated(const spice_moe_cfg_t* cfg, int32_t 
  * Step 3 with 8-bit weights and activations (cfg->wfmt SPICE_WFMT_INT8): for every HIT slot, grouped by
  * expert, and for the shared block on all T tokens
  *   g = sx * s1 * sum_k q1 qx,  u = sx * s3 * sum_k q3 qx          (int32 sums, exact)
- *   h = silu(g) u;  sh = max |h| / 127 over the row;  qh = h / sh rounded to the nearest integer
+ *   h = silu(g) u;  sh = max |h| / 127 over the row;  qh = 127 h / max |h| rounded to the nearest integer
  *   y = sh * s2 * sum_k q2 qh                                      (int32 sums, exact)
  * h, the scales and y are fp32.  A row whose x_scale or max |h| is not finite comes out NaN.
  *   x_q, x_scale  device [T][d] int8 and [T] fp32: the activations, e.g. from moe_rmsnorm_quant

@@ -96,11 +96,21 @@ __device__ __forceinline__ float max_or_nan(float a, float b) {
     return a != a || b != b ? __builtin_nanf("") : fmaxf(a, b);
 }
 
-// Codes of 4 values times inv (0: a row of zeros, or one that is not finite).
-__device__ __forceinline__ uint32_t pack_codes(const f32x4_t& v, float inv) {
+// Factors from a row's values to its codes, by its maximum: lift, a power of two and exact, keeps 127 / top finite
+// where top is tiny (below 3.7e-37 it would overflow); inv 0 for a row of zeros, or one that is not finite (top NaN).
+struct CodeScale {
+    float lift, inv;
+};
+__device__ __forceinline__ CodeScale code_scale(float top) {
+    const float lift = top < 0x1p-96f ? 0x1p+96f : 1.f;
+    return {lift, top > 0.f ? 127.f / (top * lift) : 0.f};
+}
+
+// Codes of 4 values.
+__device__ __forceinline__ uint32_t pack_codes(const f32x4_t& v, CodeScale c) {
     uint32_t bits = 0;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) bits |= (uint32_t)((int)rintf(inv == 0.f ? 0.f : v[k] * inv) & 255) << (8 * k);
+    for (int k = 0; k < 4; ++k) bits |= (uint32_t)((int)rintf(c.inv == 0.f ? 0.f : v[k] * c.lift * c.inv) & 255) << (8 * k);
     return bits;
 }
 
@@ -552,15 +562,15 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2))
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) top = max_or_nan(top, __shfl_xor(top, o));
         if (lane == 0) s_top[row] = top / 127.f;
-        const float inv = top > 0.f ? 127.f / top : 0.f;
+        const CodeScale scale = code_scale(top);
         const f32x4_t* hr = reinterpret_cast<const f32x4_t*>((j.shared ? a.hs : a.h) + (row_first + row) * j.kdim);
         uint32_t* codes = reinterpret_cast<uint32_t*>(s_lds + C::SW * C::kWTile + kOwnTops + row * own_ld);
 #pragma unroll
         for (int c = 0; c < kOwnVec; ++c) {
             const int i = v0 + lane + 64 * c;
-            if (i < v1) codes[i] = pack_codes(hv[c], inv);
+            if (i < v1) codes[i] = pack_codes(hv[c], scale);
         }
-        for (int i = v0 + lane + 64 * kOwnVec; i < v1; i += 64) codes[i] = pack_codes(hr[i], inv);
+        for (int i = v0 + lane + 64 * kOwnVec; i < v1; i += 64) codes[i] = pack_codes(hr[i], scale);
     };
     if constexpr (kOwn) {
         if (w < own_rows * segs) own_load(w);
@@ -722,12 +732,12 @@ __global__ __launch_bounds__(kQuantThreads) void i8_quant_kernel(FfnI8Args a, in
     for (int i = 1; i < kQuantThreads / 64; ++i) top = max_or_nan(top, s_top[i]);
     if (tid == 0 && seg == 0) (shared ? a.hscale_s : a.hscale)[row] = top / 127.f;
     // a row that is not finite has a maximum of NaN: codes 0, and the scale NaN
-    const float inv = top > 0.f ? 127.f / top : 0.f;
+    const CodeScale scale = code_scale(top);
 #pragma unroll
     for (int c = 0; c < kQuantVec; ++c) {
         const int i = i0 + c * kQuantThreads;
         if (i >= nv) break;
-        q[i] = pack_codes(v[c], inv);
+        q[i] = pack_codes(v[c], scale);
     }
 }
 

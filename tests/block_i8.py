@@ -111,6 +111,30 @@ def swiglu_i8_ref(xq, xs, w13, w2, d, I):
     return y, tol
 
 
+def swiglu_i8_tiny_ref(xq, xs, w13, w2, d, I):
+    """The same for rows whose h may lie below the smallest normal fp32, and max |h| of each row.
+
+    There h and the row's scale are rounded to whole steps of 2^-149, half a step each: that is what a code's
+    quotient t = 127 h / top may be off by, over top / 127 (h's share) and times t / 127 (top's), and y by half
+    a step over the scale."""
+    half = 2.0 ** -150
+    a, s = unblob(w13, 2 * I, d)
+    gu = (xq.double() @ a.t()) * xs.double()[:, None] * s
+    g, u = gu[:, :I], gu[:, I:]
+    h = g / (1 + torch.exp(-g)) * u
+    err = (16 + 5 * g.abs()) * U
+    top = h.abs().amax(1, keepdim=True)
+    eh = err.amax(1, keepdim=True)
+    t = 127 * h / top
+    q = torch.round(t)
+    off = t.abs() * (err + eh + 4 * U) + (127 + t.abs()) * half / top
+    border = (((t - torch.floor(t)) - 0.5).abs() <= off).double()
+    b, s2 = unblob(w2, d, I)
+    step = 127 * half / top  # of the scale, relative
+    y = (q @ b.t()) * (top / 127) * s2
+    return y, (border @ b.abs().t()) * (top / 127) * s2 * (1 + eh + step) + y.abs() * (eh + 8 * U + step), top[:, 0]
+
+
 def lore_ref(x, A, B):
     return x.double() @ A.double().t() @ B.double().t()
 

@@ -725,3 +725,31 @@ def test_cache_admits_8_bit_experts():
     assert torch.equal(p13[1].cpu(), t13[7]) and torch.equal(p2[1].cpu(), t2[7])
     assert slot.cpu().tolist() == [-1, -1, -1, -1, 0, -1, 2, 1]
     c.close()
+
+
+# ---- rows of H that are tiny ---------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("T,K", [(1, 2), (2, 3), (14, 2), (200, 2)])
+def test_experts_tiny_rows(T, K):
+    """Rows whose H lies below 127 / the largest fp32 (3.7e-37), down to a few thousand steps of the smallest one:
+    their codes are the nearest integers too.  W2's scales lift the outputs back to ordinary sizes."""
+    e = Experts(T, 64, 4, K, 96, 80, 4, seed=T)
+    e.xs *= 2.0 ** -(56 + (torch.arange(T, device="cuda") + 11) % 14).float()  # from 2^-67 on
+    for blob, k in [(b, 96) for b in e.w2] + [(e.w2s, 80)]:
+        blob[64 * k:] = (blob[64 * k:].clone().view(F32) * 2.0 ** 110).view(torch.uint8)
+    e.run()
+    got = e.y_slots[e.pos]
+    tops = [R.swiglu_i8_tiny_ref(e.xq, e.xs, e.w13s, e.w2s, 64, 80)[2]]
+    e.near(e.y_shared, *R.swiglu_i8_tiny_ref(e.xq, e.xs, e.w13s, e.w2s, 64, 80)[:2])
+    for x in range(4):
+        s = (e.idx.cuda().reshape(-1) == x).nonzero()[:, 0]
+        if s.numel():
+            c = int(e.slot[x])
+            y, tol, top = R.swiglu_i8_tiny_ref(e.xq[s // K], e.xs[s // K], e.w13[c], e.w2[c], 64, 96)
+            e.near(got[s], y, tol)
+            tops.append(top)
+    tops = torch.cat(tops)
+    assert (tops < 3.7e-37).any()
+    assert T < 14 or ((tops > 1e-42) & (tops < 1e-40)).any() and ((tops > 1e-38) & (tops < 3.7e-37)).any()
+    assert spice.spice_workspace_flags(e.ws, e.wsn) == 0
