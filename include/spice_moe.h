@@ -256,7 +256,7 @@ spice_status_t moe_rmsnorm_quant(const spice_moe_cfg_t* cfg, int32_t T, const vo
  * in the same launches: what lore_surrogate_apply computes, up to the order of its fp32 sums
  * (with many tokens the two may take different tiles).
  *   x, perm, offsets       as produced/consumed by moe_route_bucket
- *   resident_slot device [N] int32, as in moe_route_bucket
+ *   resident_slot device [N] int32, as in moe_route_bucket; no two experts share a slot
  *   w13_pool      device [C][2I][d]  rows 0..I-1 gate W1, rows I..2I-1 up W3 (dtype)
  *   w2_pool       device [C][d][I]   down projection (dtype)
  *   w13_shared    device [2I_s][d], w2_shared device [d][I_s]   (ignored if I_s == 0)
@@ -306,7 +306,8 @@ spice_status_t moe_expert_ffn_grouped_gated(const spice_moe_cfg_t* cfg, int32_t 
  *   w13_pool, w2_pool, w13_shared, w2_shared  device blobs (see SPICE_WFMT_INT8)
  *   w_shared_gate device [d] bf16, or NULL: as in moe_expert_ffn_grouped_gated
  *   lore_A, lore_B  as in lore_surrogate_apply, whose corrections run in the same launches, or NULL
- *   perm, offsets, resident_slot, y_slots, y_shared, ws  as in moe_expert_ffn_grouped
+ *   perm, offsets, resident_slot, y_slots, y_shared, ws  as in moe_expert_ffn_grouped; here experts
+ *                 may share a pool slot
  * Errors: as moe_expert_ffn_grouped, plus UNSUPPORTED for another wfmt or unaligned buffers (16 bytes).
  */
 spice_status_t moe_expert_ffn_grouped_i8(const spice_moe_cfg_t* cfg, int32_t T, const int8_t* x_q,

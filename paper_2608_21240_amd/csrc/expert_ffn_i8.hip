@@ -762,14 +762,16 @@ long long tiles_of(long long n, int per) { return (n + per - 1) / per; }
 template <bool kUp, class C, bool kOwn = false>
 hipError_t launch_pass(const FfnI8Args& a, const I8Plan& plan, int group, int own_bytes, hipStream_t s) {
     constexpr int feat = kUp ? C::kUpFeat : C::BM;
-    const long long slots = (long long)a.T * a.K, buckets = std::min<long long>(std::min(a.N, a.C), slots);
+    // HIT buckets at most.  Experts may share a pool slot, so there can be more than C (a grid for C of them / this, us
+    // per call with 40 and 48 of 64 experts resident: a layer's T = 16 82.4 / 81.2, T = 32 88.1 / 87.1).
+    const long long slots = (long long)a.T * a.K, buckets = a.C > 0 ? std::min<long long>(a.N, slots) : 0;
     const long long nt_sh = tiles_of(kUp ? a.Is : a.d, feat), nt_e = tiles_of(kUp ? a.I : a.d, feat);
     Job job{a, {1, 1}, kUp || !a.part ? 1 : plan.parts, 0, plan.xcd, group, (int)std::min<long long>(slots, C::BT)};
     const long long lore_b = a.r > 0 ? std::min<long long>(a.N, slots) : 0;
     const long long lore = lore_b ? (slots / C::BT + lore_b) * tiles_of(kUp ? a.r : a.d, kUp ? C::BM : C::BM * kLoreDown) : 0;
-    // upper bound: sum_e ceil(n_e / BT) <= slots / BT + buckets; blocks past the live tiles exit
+    // upper bound: sum_e ceil(n_e / BT) <= buckets + (slots - buckets) / BT; blocks past the live tiles exit
     const long long tiles = (a.Is > 0 ? tiles_of(a.T, C::BT) * nt_sh * job.parts : 0) +
-                            (buckets > 0 ? (slots / C::BT + buckets) * nt_e : 0) + lore;
+                            (buckets > 0 ? (buckets + (slots - buckets) / C::BT) * nt_e : 0) + lore;
     if (tiles == 0) return hipSuccess;
     if (tiles > 0x7FFFFFFFll) return hipErrorInvalidValue;
     job.lore = (int32_t)lore;

@@ -753,3 +753,15 @@ def test_experts_tiny_rows(T, K):
     assert (tops < 3.7e-37).any()
     assert T < 14 or ((tops > 1e-42) & (tops < 1e-40)).any() and ((tops > 1e-38) & (tops < 3.7e-37)).any()
     assert spice.spice_workspace_flags(e.ws, e.wsn) == 0
+
+
+@pytest.mark.parametrize("T,C", [(1, 2), (3, 2), (17, 1), (60, 2), (400, 3)])
+def test_experts_that_share_pool_slots(T, C):
+    """More experts than pool slots, all resident: several of them have one slot's weights."""
+    e = Experts(T, 80, 40, 4, 48, 32, C, seed=T)
+    e.slot = (torch.arange(40, dtype=torch.int32) % C).cuda()
+    e.cls = torch.full_like(e.cls, HIT)
+    perm, inv, off = R.buckets_ref(e.idx.numpy(), e.cls.numpy(), 40)
+    e.perm, e.offsets, e.pos = torch.from_numpy(perm).int().cuda(), torch.from_numpy(off).int().cuda(), torch.from_numpy(inv).cuda()
+    e.run()
+    e.check()
