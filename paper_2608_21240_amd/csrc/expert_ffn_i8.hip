@@ -152,19 +152,24 @@ struct Tile {
 };
 
 // The bucket of class c holding tile L of nt tiles per token tile, by a wave's scan of the offsets; slot:
-// its pool slot (class HIT).
+// its pool slot (class HIT).  A bucket outside the slots raises a flag and has no tiles, so it takes none of
+// the grid's from the others.
 __device__ bool find_bucket(const FfnI8Args& a, int c, int nt, int BT, int& L, int lane, int& e_, int& st_, int& n_,
                             int& slot_) {
     const int32_t* off = a.offsets + c * (a.N + 1);
+    const uint32_t slots = (uint32_t)(a.T * a.K);
     for (int e0 = 0; e0 < a.N; e0 += 64) {
         const int e = e0 + lane;
         int st = 0, n = 0, slot = -1;
         if (e < a.N) {
             st = off[e];
-            n = off[e + 1] - st;
+            n = (int)((uint32_t)off[e + 1] - (uint32_t)st);
             if (c == SPICE_CLASS_HIT) slot = a.resident_slot[e];
+            if ((uint32_t)st > slots || (uint32_t)n > slots - (uint32_t)st) {  // not inside the T K slots: no tiles
+                atomicOr(&a.ctrl[kWordFlags], (uint32_t)SPICE_FLAG_BAD_INDEX);
+                n = 0;
+            }
         }
-        if (n > a.T * a.K) n = 0;
         const int tiles = n > 0 ? ((n + BT - 1) / BT) * nt : 0;
         int incl = tiles;
 #pragma unroll
@@ -264,10 +269,6 @@ __device__ bool resolve(const Job& job, int L, Tile& j) {
         j.kdim = kUp ? a.d : a.I;
         j.nfeat = kUp ? a.I : a.d;
         j.up_off = j.nfeat;
-    }
-    if (st < 0 || st > a.T * a.K - n) {
-        if (threadIdx.x == 0) atomicOr(&a.ctrl[kWordFlags], (uint32_t)SPICE_FLAG_BAD_INDEX);
-        return false;
     }
     const int mt = (n + C::BT - 1) / C::BT, rows = !j.lore ? feat : kUp ? C::BM : C::BM * kLoreDown;
     if (job.xcd) {
@@ -711,7 +712,7 @@ __global__ __launch_bounds__(kQuantThreads) void i8_quant_kernel(FfnI8Args a, in
     const bool shared = (int)blockIdx.x < nsh * segs_sh;
     const int b = shared ? blockIdx.x : blockIdx.x - nsh * segs_sh, per = shared ? segs_sh : segs;
     const int row = b / per, seg = b - row * per;
-    if (!shared && row >= a.offsets[a.N]) return;  // the HIT buckets' end
+    if (!shared && (uint32_t)row >= (uint32_t)a.offsets[a.N]) return;  // the HIT buckets' end
     const int tid = threadIdx.x, n = shared ? a.Is : a.I, nv = n / 4, nt = (n + group - 1) / group;
     const f32x4_t* h = reinterpret_cast<const f32x4_t*>((shared ? a.hs : a.h) + (size_t)row * n);
     const float* part = (shared ? a.top_s : a.top) + (size_t)row * (n / 16);

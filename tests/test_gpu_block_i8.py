@@ -765,3 +765,41 @@ def test_experts_that_share_pool_slots(T, C):
     e.perm, e.offsets, e.pos = torch.from_numpy(perm).int().cuda(), torch.from_numpy(off).int().cuda(), torch.from_numpy(inv).cuda()
     e.run()
     e.check()
+
+
+@pytest.mark.parametrize("T", [1, 40, 300])
+@pytest.mark.parametrize("c", [HIT, LORE])
+@pytest.mark.parametrize("bad", [1 << 30, -1, -(1 << 31)])
+@pytest.mark.parametrize("at", [3, 6])
+def test_a_bucket_of_impossible_size_raises_a_flag(T, c, bad, at):
+    """A start that gives one bucket more than T K slots, or the one before it fewer than none: the flag is raised,
+    the two are skipped and every other bucket's rows are right."""
+    N, K, r = 6, 4, 8
+    e = Experts(T, 64, N, K, 48, 32, N if c == HIT else 0, r=r, seed=T, lore=True)
+    e.offsets[c, at] = bad  # the end of a bucket and the start of the next (or the class's end)
+    e.run(lore=True)
+    assert spice.spice_workspace_flags(e.ws, e.wsn, clear=True) == spice.SPICE_FLAG_BAD_INDEX
+    e.near(e.y_shared, *R.swiglu_i8_ref(e.xq, e.xs, e.w13s, e.w2s, 64, 32))
+    got = e.y_slots[e.pos]
+    for x in range(N):
+        s = (e.idx.cuda().reshape(-1) == x).nonzero()[:, 0]
+        if s.numel() == 0:
+            continue
+        if x in (at - 1, at):
+            assert (got[s] == 7).all()
+        elif c == HIT:
+            i = int(e.slot[x])
+            e.near(got[s], *R.swiglu_i8_ref(e.xq[s // K], e.xs[s // K], e.w13[i], e.w2[i], 64, 48))
+        else:
+            y = R.lore_ref(e.x[s // K], e.lore_A[x], e.lore_B[x])
+            e.near(got[s], y, 1e-4 * y.abs().amax(1, keepdim=True))
+
+
+@pytest.mark.parametrize("T", [1, 40, 300])
+def test_bad_starts_raise_a_flag(T):
+    """Buckets of right sizes past the end of the slots."""
+    for c in (HIT, LORE):
+        e = Experts(T, 64, 4, 2, 48, 32, 4 if c == HIT else 0, r=8, seed=3, lore=True)
+        e.offsets[c, 1:] += T * 2
+        e.run(lore=True)
+        assert spice.spice_workspace_flags(e.ws, e.wsn, clear=True) == spice.SPICE_FLAG_BAD_INDEX
