@@ -203,7 +203,9 @@ class LayerRun:
             raise ValueError(f"invalid configuration for the library: {spice.last_error()}")
         self.ws = torch.zeros(self.ws_bytes, dtype=torch.uint8, device=device)
         # what the norm in front of the layer leaves: residual stream, normed rows, 8-bit rows and their scales
+        # (of the first `normed` tokens)
         self.h = self.y = self.x_q = self.x_scale = None
+        self.normed = 0
         if wfmt == WFMT_INT8:
             self.x_q = torch.empty((T, d), dtype=torch.int8, device=device)
             self.x_scale = torch.empty(T, **f32)
@@ -252,6 +254,7 @@ class LayerRun:
             self.h = torch.empty((self.T, self.shape.d), dtype=torch_dtype(self.shape.dtype), device=x.device)
             self.y = torch.empty_like(self.h)
         spice.moe_rmsnorm_quant(self.cfg, T, x, resid, weight, eps, self.h, self.y, self.x_q, self.x_scale)
+        self.normed = T
         return self.y
 
     def route(self, L: DeviceLayer, x: torch.Tensor, conf: Optional[torch.Tensor], T: Optional[int] = None,
@@ -295,10 +298,13 @@ class LayerRun:
         self.wait_ready = to_host
 
     def experts(self, L: DeviceLayer, x: torch.Tensor, T: Optional[int] = None, fuse_lore: bool = True):
+        """The expert FFN on x; 8-bit experts take the 8-bit rows of the last norm(), whose rows x has to be."""
         T = self.T if T is None else T
         self._same_format(L)
         la, lb = (L.lore_A, L.lore_B) if fuse_lore else (None, None)
         if self.cfg.wfmt == WFMT_INT8:
+            if x is None or self.y is None or self.normed < T or x.data_ptr() != self.y.data_ptr():
+                raise ValueError("8-bit experts take the rows of the last norm(): call it first and pass what it returns")
             spice.moe_expert_ffn_grouped_i8(self.cfg, T, self.x_q, self.x_scale, x, self.perm, self.offsets,
                                             L.resident_slot, L.w13_pool, L.w2_pool, L.w13s, L.w2s, L.w_sg, la, lb,
                                             self.y_slots, self.y_shared, self.ws, self.ws_bytes)

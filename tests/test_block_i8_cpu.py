@@ -187,6 +187,35 @@ def test_layer_driver_asks_for_the_norm():
         run.layer_gpu(type("L", (), {"wfmt": 0})(), None, None)
 
 
+def test_experts_take_only_the_rows_of_the_last_norm(monkeypatch):
+    """The 8-bit rows belong to the rows that norm() returned: other rows, none yet, or more of them are refused."""
+    torch = pytest.importorskip("torch")
+    from paper_2608_21240_amd import layer as LY
+
+    calls = []
+    monkeypatch.setattr(spice, "moe_rmsnorm_quant", lambda *a: None)
+    monkeypatch.setattr(spice, "moe_expert_ffn_grouped_i8", lambda *a: calls.append(a))
+    run = LY.LayerRun.__new__(LY.LayerRun)
+    run.T, run.cfg, run.shape, run.normed = 4, cfg(), S, 0
+    run.h = run.y = None
+    run.x_q, run.x_scale = torch.empty(4, 256, dtype=torch.int8), torch.empty(4)
+    for name in ("perm", "offsets", "y_slots", "y_shared", "ws", "ws_bytes"):
+        setattr(run, name, None)
+    L = type("L", (), dict.fromkeys(("resident_slot", "w13_pool", "w2_pool", "w13s", "w2s", "w_sg", "lore_A", "lore_B")))()
+    L.wfmt = W.WFMT_INT8
+    x = torch.randn(4, 256).to(torch.bfloat16)
+    with pytest.raises(ValueError, match="norm"):
+        run.experts(L, x)
+    y = run.norm(x, None, None, 1e-6, T=3)
+    run.experts(L, y, 3)
+    run.experts(L, y[:2], 2)
+    assert [a[1] for a in calls] == [3, 2] and all(a[2] is run.x_q for a in calls)
+    for rows, T in ((x, 3), (y[1:], 2), (y, 4), (None, 3)):
+        with pytest.raises(ValueError, match="norm"):
+            run.experts(L, rows, T)
+    assert len(calls) == 2
+
+
 # ---- the rules that pick a call's kernels ------------------------------------------------------
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
