@@ -198,10 +198,10 @@ constexpr size_t kTiledBucketLds = bucket_lds_bytes(kPrefillThreads, SPICE_MAX_E
 // contraction; the last of the group's blocks adds the parts in order), top-K, gates, classes.
 // kOne: the last block over all groups then buckets the slots (few tokens); otherwise the
 // group's histogram of bucket keys goes to column b / blocks of the table.
-// kScored: a group's blocks also share the experts, `chunk` each (whole groups of expert tiles), 64 or more,
+// kScored: a group's blocks also share the experts, `chunk` each (scored_plan), 64 or more but for the last,
 // which leaves fewer partial logits for its last block to add and busies more CUs (one chunk / this, us per
 // call: N = 256, d = 3584, T = 120 43 / 30, T = 250 46 / 35, T = 500 51 / 47; N = 128 the same).
-constexpr int kChunkExperts = 64;
+static_assert(kChunkAlign == 16 * kGroupTiles, "a chunk is whole groups of expert tiles");
 template <int DT, bool kOne, bool kScored>
 __global__ __launch_bounds__(kPrefillThreads) void route_tiled_kernel(RouteArgs a, int parts_k, int chunks_n, int chunk) {
     __shared__ __align__(16) unsigned char s_raw[sizeof(PrefillLds) > kTiledBucketLds ? sizeof(PrefillLds) : kTiledBucketLds];
@@ -508,24 +508,17 @@ hipError_t launch_scored_rows(const RouteArgs& a, hipStream_t s) {
 template <int DT, bool kScored>
 hipError_t launch_route(const RouteArgs& a, hipStream_t s) {
     const unsigned groups = (unsigned)((a.T + kPrefillTok - 1) / kPrefillTok);
-    int parts = route_parts(a.T, a.N, a.d, a.dtype, a.part_bytes);
-    if ((kScored ? scored_keeps_rows : route_keeps_rows)(a.T, a.N, a.d, parts, a.hx != nullptr)) {
-        if constexpr (kScored) return launch_scored_rows<DT>(a, s);
-        const int g = route_blocks_per_token(a.N + (a.w_sg ? 1 : 0), kLogitThreads);
-        hipLaunchKernelGGL(route_logits_kernel<DT>, dim3((unsigned)(a.T * g)), dim3(kLogitThreads), 0, s, a, g);
-        return hipGetLastError();
-    }
-    int chunks = 1, chunk = a.N;
-    if (kScored && parts > 1) {  // a block per CU at most, experts before parts of the contraction
-        const int per_group = (int)(256 / groups);  // at least parts
-        constexpr int kAlign = 16 * kGroupTiles;
-        const int want = a.N / kChunkExperts;
-        const int wide = want > 1 ? ((a.N + want - 1) / want + kAlign - 1) / kAlign * kAlign : a.N;
-        // where they come out uneven, the widest takes longer than the parts saved (N = 130, T = 1000 37 / 40 us)
-        if (want > 1 && want <= per_group && 4 * want * wide <= 5 * a.N) {
-            chunk = wide;
-            chunks = (a.N + wide - 1) / wide;
-            parts = std::max(1, std::min(parts, per_group / chunks));
+    int parts, chunks = 1, chunk = a.N;
+    if constexpr (kScored) {
+        const ScoredPlan p = scored_plan(a.T, a.N, a.d, a.dtype, a.part_bytes, a.hx != nullptr);
+        if (p.rows) return launch_scored_rows<DT>(a, s);
+        parts = p.parts; chunks = p.chunks; chunk = p.chunk;
+    } else {
+        parts = route_parts(a.T, a.N, a.d, a.dtype, a.part_bytes);
+        if (route_keeps_rows(a.T, a.N, a.d, parts, a.hx != nullptr)) {
+            const int g = route_blocks_per_token(a.N + (a.w_sg ? 1 : 0), kLogitThreads);
+            hipLaunchKernelGGL(route_logits_kernel<DT>, dim3((unsigned)(a.T * g)), dim3(kLogitThreads), 0, s, a, g);
+            return hipGetLastError();
         }
     }
     const dim3 grid(groups * (unsigned)(parts * chunks));

@@ -67,6 +67,28 @@ inline bool scored_keeps_rows(int32_t T, int32_t N, int32_t d, int parts, bool x
     if (T > kRouteTokenMaxT || (int64_t)T * N >= kScoredTiledMinSlots) return false;
     return !x_to_host || route_keeps_rows(T, N, d, parts, x_to_host);
 }
+// A scored routing call: rows, or tiles in `parts` parts of the contraction whose groups' blocks also share the
+// experts, `chunk` each in `chunks` chunks.  Experts come before parts, a block per CU at most; a chunk is whole
+// groups of expert tiles.  Where they come out uneven, the widest chunk takes longer than the parts saved (N = 130,
+// T = 1000 37 / 40 us).
+constexpr int kChunkExperts = 64, kChunkAlign = 32;
+struct ScoredPlan {
+    int rows, parts, chunks, chunk;
+};
+inline ScoredPlan scored_plan(int32_t T, int32_t N, int32_t d, int32_t dtype, size_t part_bytes, bool x_to_host) {
+    ScoredPlan p{0, route_parts(T, N, d, dtype, part_bytes), 1, N};
+    p.rows = scored_keeps_rows(T, N, d, p.parts, x_to_host);
+    if (p.rows || p.parts <= 1) return p;
+    const int per_group = 256 / ((T + kRouteTileTok - 1) / kRouteTileTok);  // blocks, at least parts
+    const int want = N / kChunkExperts;
+    if (want <= 1 || want > per_group) return p;
+    const int wide = ((N + want - 1) / want + kChunkAlign - 1) / kChunkAlign * kChunkAlign;
+    if (4 * want * wide > 5 * N) return p;
+    p.chunk = wide;
+    p.chunks = (N + wide - 1) / wide;
+    p.parts = std::max(1, std::min(p.parts, per_group / p.chunks));
+    return p;
+}
 static_assert((kWordTokCount + kRouteTokenMaxT * kTokCountStride) * 4 <= SPICE_WS_CONTROL_BYTES, "control region too small");
 // [T*K] bucket keys (class * N + expert) of the decode routing call's slots, written through
 // to the device-coherent level for the block that buckets them (top-K of 64 at most)

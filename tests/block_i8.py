@@ -148,3 +148,12 @@ SHAPE_CALLS = [
 SPLIT_CALLS = [
     ((1, 64, 4, 1, 16, 8192, 1), 4), ((70, 208, 4, 2, 32, 4112, 2), 2), ((3, 4096, 8, 2, 48, 16400, 8), 8),
     ((500, 128, 4, 1, 64, 6160, 0), 3), ((1, 64, 4, 1, 16, 4080, 1), 1)]
+
+# Calls (T, d, N, K, fp32) of the scored routing that run in tiles with the whole workspace: the blocks of 16 tokens
+# split the contraction in so many parts and share the experts in so many chunks of so many.
+SCORED_TILES = [
+    ((120, 2048, 256, 8, False), (8, 4, 64)), ((250, 2048, 256, 8, False), (4, 4, 64)),   # one launch
+    ((250, 1024, 100, 6, True), (8, 1, 100)), ((150, 512, 160, 4, False), (4, 2, 96)),
+    ((300, 2048, 191, 3, False), (6, 2, 96)), ((300, 2048, 130, 3, False), (8, 1, 130)),  # an uneven chunk, one refused
+    ((257, 1040, 192, 64, True), (5, 3, 64)), ((1000, 4096, 256, 8, False), (1, 4, 64)),  # chunks alone
+    ((2000, 2048, 128, 8, False), (1, 2, 64))]

@@ -292,3 +292,62 @@ def test_the_workspace_has_the_split_tiles_sums(plan):
         a, b = (spice.spice_workspace_bytes(cfg(W.MoEShape(d, N, K, I, s, 0, W.DTYPE_BF16), n_slots=C), T) for s in (Is, 16))
         rows = T * ((Is - 16) * 4 + (Is - 16) // 16 * 4)  # H and its partial maxima
         assert a - b >= rows + plan((T, d, N, K, C, I, Is))[0][3]
+
+
+@pytest.fixture(scope="module")
+def scored(tmp_path_factory):
+    """scored(calls of T, N, d, dtype, part_bytes, x_to_host) -> (rows kept, parts, chunks, experts per chunk) of each."""
+    if not shutil.which("g++") or not os.path.exists(os.path.join(ROCM, "include", "hip", "hip_runtime_api.h")):
+        pytest.skip("g++ or the HIP headers are not installed")
+    exe = str(tmp_path_factory.mktemp("scored") / "driver")
+    subprocess.run(["g++", "-std=c++17", "-O1", f"-I{ROOT}/include", f"-I{ROOT}/paper_2608_21240_amd/csrc",
+                    f"-I{ROCM}/include", "-D__HIP_PLATFORM_AMD__", os.path.join(ROOT, "tests", "route_plan_driver.cpp"),
+                    "-o", exe], check=True)
+
+    def ask(*calls):
+        text = "".join(" ".join(str(int(v)) for v in c) + "\n" for c in calls)
+        r = subprocess.run([exe], input=text, capture_output=True, text=True, check=True)
+        out = [tuple(map(int, ln.split())) for ln in r.stdout.splitlines()]
+        assert len(out) == len(calls)
+        return out
+
+    return ask
+
+
+WHOLE = 1 << 40
+
+
+def test_scored_calls_reach_their_tiles(scored):
+    """The calls of the GPU test: with the workspace's optional end the parts and chunks they are named for, without
+    it neither."""
+    for (T, d, N, K, f32), tiles in R.SCORED_TILES:
+        dtype = W.DTYPE_F32 if f32 else W.DTYPE_BF16
+        whole, base = scored((T, N, d, dtype, WHOLE, 0), (T, N, d, dtype, 0, 0))
+        assert whole == (0, *tiles) and base == (0, 1, 1, N)
+        c = cfg(W.MoEShape(d, N, K, 96, 160, 8, dtype), wfmt=0)
+        # what the parts take is there
+        assert spice.spice_workspace_bytes(c, T) - spice.SPICE_WS_CONTROL_BYTES >= tiles[0] * -(-T // 16) * 16 * N * 8
+
+
+def test_scored_rows_and_tiles(scored):
+    """Rows up to 256 tokens and 24000 token-expert pairs, with x to the host where the plain call keeps them too."""
+    bf = W.DTYPE_BF16
+    got = scored((93, 256, 3584, bf, WHOLE, 0), (94, 256, 3584, bf, WHOLE, 0), (256, 93, 128, bf, WHOLE, 0),
+                 (257, 16, 128, bf, WHOLE, 0), (230, 64, 2048, bf, WHOLE, 1), (200, 64, 2048, bf, WHOLE, 1))
+    assert [g[0] for g in got] == [1, 0, 1, 0, 0, 1]
+
+
+def test_scored_plans_stay_within_their_limits(scored):
+    r = random.Random(5)
+    calls = [(int(2 ** r.uniform(0, 16)), r.randint(1, 256), 8 * r.randint(1, 512), r.randint(0, 1), r.choice([0, 1 << 16, 1 << 20, WHOLE]),
+              r.randint(0, 1)) for _ in range(6000)]
+    for (T, N, d, dtype, room, host), (rows, parts, chunks, chunk) in zip(calls, scored(*calls)):
+        groups = -(-T // 16)
+        if rows:
+            assert T <= 256
+            continue
+        assert 1 <= parts <= 8 and (chunks - 1) * chunk < N <= chunks * chunk  # every chunk has experts
+        assert chunks == 1 or chunk % 32 == 0 and chunk >= 64
+        if parts * chunks > 1:
+            # a counter per group, the partial logits in their room, a block per CU
+            assert groups <= 256 and parts * groups * 16 * N * 8 <= room and groups * parts * chunks <= 256

@@ -803,3 +803,29 @@ def test_bad_starts_raise_a_flag(T):
         e.offsets[c, 1:] += T * 2
         e.run(lore=True)
         assert spice.spice_workspace_flags(e.ws, e.wsn, clear=True) == spice.SPICE_FLAG_BAD_INDEX
+
+
+# ---- scored routing in tiles: contractions and experts split over a group's blocks -----------------
+
+
+@pytest.mark.parametrize("rule", [0, 2])
+@pytest.mark.parametrize("size,tiles", R.SCORED_TILES)
+def test_scored_routing_in_split_tiles(size, tiles, rule):
+    """Long rows and many experts, on the whole workspace (twice: its counters are back at zero) and on the smallest
+    one, which leaves no room for partial logits."""
+    T, d, N, K, f32 = size
+    say("route", size, tiles)
+    rule = RULES[rule] if N % 4 == 0 and K <= N // 2 else dict(RULES[rule], groups=1, keep=1)
+    r = Routing(T, d, N, K, F32 if f32 else BF, C=N // 3, seed=T + N, norm_topk=1)
+    z = r.x.double() @ r.wg.double().t()
+    room = float(2 * d * 2.0 ** -53 * (r.x.double().abs() @ r.wg.double().abs().t()).max())
+    full, r.wsn = r.wsn, 1024
+    with pytest.raises(spice.SpiceError) as e:
+        r.run(**rule)
+    base = int(str(e.value).split("needs ")[1].split()[0].rstrip(")"))
+    assert base < full
+    for r.wsn in (full, full, base):
+        r.logits.fill_(9), r.idx.fill_(-9), r.perm.fill_(-9)
+        r.run(**rule)
+        assert torch.allclose(r.logits, z, rtol=0, atol=room)
+        r.check(r.logits.cpu().numpy(), **rule)
