@@ -215,7 +215,8 @@ typedef struct {
  *   topk_w = g * scale; the confidence modes GATE and GATE_RENORM read g.
  * All of it is computed in fp64 from fp64 logits; topk_w is rounded once.  A logit of -inf (through
  * logit_bias) masks its expert: its score is 0, it counts in no group value, and it is chosen, with
- * weight 0, only when a token's kept groups have fewer than K others.  Weights whose sum is 0 stay 0.
+ * weight 0, only when a token's kept groups have fewer than K others.  A balance_bias of -inf does the
+ * same, but the weight is the expert's score.  Weights whose sum is 0 stay 0.
  * Logits that are NaN or +inf give valid experts and unspecified weights.
  *   score   host struct; N must be a multiple of n_group and topk_group * N/n_group at least K
  *   logits  device [T][N] fp64 out, or NULL: z, as in moe_route_bucket

@@ -829,3 +829,19 @@ def test_scored_routing_in_split_tiles(size, tiles, rule):
         r.run(**rule)
         assert torch.allclose(r.logits, z, rtol=0, atol=room)
         r.check(r.logits.cpu().numpy(), **rule)
+
+
+@pytest.mark.parametrize("T", [4, 215, 300])
+@pytest.mark.parametrize("rule", [RULES[2], RULES[3]])
+def test_infinite_balance_biases(T, rule):
+    """-inf: chosen only where a token's kept groups have fewer than K others, in no group value, the weight its
+    score; +inf: first."""
+    r = Routing(T, 64, 48, 5, C=9, seed=4)
+    for low in ([0, 5, 30], list(range(0, 24)), list(range(1, 48)), list(range(48))):
+        r.balance = (0.05 * torch.randn(48, generator=R.gen(8)))
+        r.balance[low] = -float("inf")
+        if len(low) == 3:
+            r.balance[[7, 8, 40]] = float("inf")
+        r.balance = r.balance.cuda()
+        r.run(**rule)
+        r.check(r.logits.cpu().numpy(), **rule)
