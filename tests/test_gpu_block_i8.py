@@ -845,3 +845,41 @@ def test_infinite_balance_biases(T, rule):
         r.balance = r.balance.cuda()
         r.run(**rule)
         r.check(r.logits.cpu().numpy(), **rule)
+
+
+@pytest.mark.parametrize("T,N,d", [(40, 48, 64), (230, 64, 2048), (250, 16, 2048), (120, 256, 1024), (250, 256, 2048)])
+def test_scored_routing_copies_to_the_host_in_one_launch(T, N, d):
+    """Rows of many slots, and the one-launch tiles, whole and split."""
+    r = Routing(T, d, N, 5, C=9, seed=2)
+    pin = lambda t: torch.zeros(t.shape, dtype=t.dtype).pin_memory()  # noqa: E731
+    x, idx, w, cls = (pin(t) for t in (r.x, r.idx, r.w, r.cls))
+    counts, ready = (torch.zeros(n, dtype=torch.int32).pin_memory() for n in (4, 1))
+    rule = dict(sigmoid=True, groups=4, keep=2)
+    r.run(**rule, host_out=spice.host_out(x, idx, w, cls, counts, ready, 78))
+    torch.cuda.synchronize()
+    r.check(r.logits.cpu().numpy(), **rule)
+    for a, b in ((x, r.x), (idx, r.idx), (w, r.w), (cls, r.cls)):
+        assert torch.equal(a, b.cpu())
+    assert counts[:3].tolist() == torch.bincount(r.cls.flatten().long(), minlength=3).tolist() and ready.item() == 78
+
+
+@pytest.mark.parametrize("size,parts", [R.SPLIT_CALLS[0], R.SPLIT_CALLS[1]])
+def test_gate_of_a_split_shared_block(size, parts):
+    e = Experts(*size, seed=5)
+    e.w_sg = (0.05 * torch.randn(e.d, generator=R.gen(9))).to(BF).cuda()
+    e.run()
+    e.check()
+
+
+@pytest.mark.parametrize("T", [1, 40])
+def test_longest_contraction(T):
+    """inter and shared_inter at their limit, every product of W2's at its largest: the sums stay in 32 bits."""
+    I = 131056
+    e = Experts(T, 16, 1, 1, I, I, 1, seed=1)
+    e.xq[:] = 127
+    for w13, w2 in ((e.w13[0], e.w2[0]), (e.w13s, e.w2s)):
+        w13[:2 * I * 16] = 127  # codes
+        w13[2 * I * 16:] = torch.full((2 * I,), 1e-3).cuda().view(torch.uint8)
+        w2[:I * 16] = 128  # code -128
+    e.run()
+    e.check()
