@@ -125,9 +125,11 @@ enum { SPICE_WFMT_DTYPE = 0, SPICE_WFMT_MXFP4 = 2, SPICE_WFMT_INT8 = 3 };
 /* Bytes of device workspace for a call with T tokens (every entry point below accepts the same
  * workspace).  Returns 0 for an invalid cfg or T.
  * The end of it is optional, a call without it only takes longer: the partial results of split
- * contractions, of the routing's logits (at most 32 KiB x N) and, behind them, of the shared block's
- * down projection (at most 8 x T x d fp32; without them y_shared differs by the order of its fp32
- * sums.  With 8-bit experts at most 16 MiB of int32, and no difference).  A SPICE_ERR_WORKSPACE message names the smallest size that the call accepts. */
+ * contractions, of the routing's logits (at most 32 KiB x N, from 208 tokens on and, for
+ * moe_route_bucket_scored alone, from 24000 token-expert pairs on) and, behind them, of the shared
+ * block's down projection (at most 8 x T x d fp32; without them y_shared differs by the order of its
+ * fp32 sums.  With 8-bit experts at most 16 MiB of int32, and no difference).  A SPICE_ERR_WORKSPACE
+ * message names the smallest size that the call accepts. */
 size_t spice_workspace_bytes(const spice_moe_cfg_t* cfg, int32_t T);
 
 /* Zero the control region of a device workspace (a fill kernel on `stream`). */

@@ -29,9 +29,9 @@
 // weights' way from memory, by which a call of 32 tokens (DeepSeek-V2-Lite sizes, 48 of 64 experts resident,
 // about 410 MB of weights) takes 83 us, its up launch at 5.4 TB/s of the 6.25 that a plain read reaches; one token
 // (43 MB) the launches' starts and ends, 17 us; long buckets the matrix units (Qwen2 sizes, T = 4096, 3.6
-// TOP: 2000 us with up at 1.96 and down at 1.80 POP/s, where a plain int8 product of 8192^3 reaches 2.13).
-// In between (T = 1000, 152 us) neither: 2.75 rounds of blocks, 115 us even where every expert has the same
-// weights, which L2 then holds.
+// TOP: 2000 us with up at 1.95 and down at 1.80 POP/s, where a plain int8 product of 8192^3 reaches 2.13; the
+// matrix units are busy for 46 and 43 % of the SIMDs' cycles).  In between (T = 1000, 152 us) neither: 2.75 rounds of
+// blocks, matrix units busy for 16 and 14 %, 115 us even where every expert has the same weights, which L2 then holds.
 // Kernels that kept a few tokens' rows in registers and streamed the weights past them, and weights and tokens
 // loaded by different waves, were not faster for any T.
 #include <hip/hip_runtime.h>
@@ -702,8 +702,8 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2))
 // Rows of H to 8 bits: a block per kQuantRow values of a row, the T shared rows first, then the HIT slots'
 // positions.  The row's maximum comes from the partial maxima that the up tiles left, one per `group`
 // features, so a row's blocks need not wait for each other; the values are on their way meanwhile.  Bound by
-// memory: Qwen2 sizes, T = 4096, 671 MB read and 168 MB written in 147 us, 5.7 TB/s; a few rows take 3 us, a
-// launch's own time. 
+// memory: Qwen2 sizes, T = 4096, 671 MB read and 168 MB written in 148 us, 5.7 TB/s; a few rows take 4 us, little
+// more than a launch's own time.
 constexpr int kQuantThreads = 256;
 constexpr int kQuantVec = 4;  // 16-byte chunks per thread
 constexpr int kQuantRow = kQuantVec * 4 * kQuantThreads;

@@ -7,9 +7,10 @@
 // sum of squares and max |a|, and a second one, over the same registers, writes every output.
 // Everything is fp64 until the one rounding of each output, so a code is the nearest integer of the exact
 // quotient.  Each byte is read and written once: memory's rate is the bound of many rows (bf16, 8192 x 3584
-// with a residual and all outputs, 264 MB: 59.6 us, 4.43 TB/s; a copy runs at 4.96), the launch and one trip
-// to memory that of a few (1 x 2048: 3.1 us).  A chunk per thread, so that none idles through a second round,
-// and cheaper conversions took the first from 72.7 us.
+// with a residual and all outputs, 264 MB: 54 us, 4.9 TB/s, a copy's rate on the same card; call after call in a
+// graph 57 us, with the time between two launches), the launch and one trip to memory that of a few (1 x 2048:
+// 2.6 us, in a graph 3.0).  A chunk per thread, so that none idles through a second round, and cheaper conversions
+// took the first from 73 us in a graph.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -139,9 +140,10 @@ __global__ __launch_bounds__(kWaveRows ? 256 : 1024) void rmsnorm_quant_kernel(N
         static_cast<uint4*>(a.y)[at] = R::pack(y);
     }
     if (!a.q) return;
-    // p * (127 / max) is off by a few units in the last place: where that can decide between two codes (bf16
-    // rows hold exact halves), the one rounding of 127 p / max does
-    double inv = __builtin_amdgcn_rcp(top);  // and a step of Newton's: within 1e-15
+    // p * (127 / max) is off by 2e-12 at most: where that can decide between two codes (bf16 rows hold exact
+    // halves), the one rounding of 127 p / max does.  v_rcp_f64 is documented to 2^29 units in the last place,
+    // 2^-23 relative; a step of Newton's squares that, 1.4e-14, on quotients of up to 127
+    double inv = __builtin_amdgcn_rcp(top);
     inv = top > 0.0 ? 127.0 * fma(fma(-top, inv, 1.0), inv, inv) : 0.0;
     int q[V];
     bool near = false;

@@ -58,7 +58,8 @@ inline bool route_keeps_rows(int32_t T, int32_t N, int32_t d, int parts, bool x_
     return x_to_host ? N >= 128 && d > 16 * T * parts : N < 56 || d > 4 * T * parts;
 }
 // The same for a scoring rule, whose tiles rank a token by one wave with few compares and share many experts
-// between blocks, and whose rows take 8 waves per block: by the ranks' and logits' number T N.  Rows / tiles, us
+// between blocks, and whose rows take 8 waves per block: by the ranks' and logits' number T N.  d moves the border
+// too, so close to it the rule is up to 2.5 us off (d = 2048, T = 96 and d = 4096, T = 160 below).  Rows / tiles, us
 // per call: N = 256, d = 3584, T = 64 (16 k) 26.4 / 29.7, T = 96 (25 k) 35.8 / 30.0, T = 207 61 / 34; d = 2048,
 // T = 96 28.2 / 29.7, T = 128 32.0 / 30.2; N = 128, d = 2048, T = 160 (20 k) 24.1 / 26.1, T = 207 (26 k) 26.8 /
 // 26.4; d = 4096, T = 160 29.1 / 26.6; N = 64, d = 2048, T = 250 (16 k) 19.1 / 23.2.
@@ -246,7 +247,8 @@ constexpr I8Shape kI8Shapes[4] = {{64, 32, 49152}, {128, 64, 73728}, {128, 128, 
 //   T = 130 (n = 12) 98 / 96, T = 219 (n = 20) 107 / 99 / 113 / 134, T = 400 (n = 37) 139 / 116 / 121 / 137,
 //   T = 700 (n = 65) 180 / 146 / 134 / 149, T = 1000 (n = 93) 231 / 169 / 150 / 163, all resident T = 1400
 //   (n = 131) 365 / 255 / 237 / 238, T = 2000 (n = 187) 490 / 329 / 293 / 278; Qwen2 sizes T = 300 (n = 37) 617 /
-//   481 / 470 / 560, T = 500 (n = 62) 824 / 594 / 530 / 600, T = 1000 (n = 125) 1418 / 895 / 738 / 709.  Small
+//   481 / 470 / 560 (the border for n = 37 is DeepSeek-V2-Lite's: 2 % too late here), T = 500 (n = 62) 824 / 594 /
+//   530 / 600, T = 1000 (n = 125) 1418 / 895 / 738 / 709.  Small
 //   layers (d, experts, their inter, shared inter; up blocks): 1024, 8, 512, 1024, T = 500 26 (1024) / 22 (256)
 //   / 26 (128) / 51 (32); 1024, 4, 1024, 1024, T = 1000 49 / 37 (768) / 34 (384) / 58 (96).
 // parts: splits of the shared block's down contraction where its tiles would outlast the routed ones (Qwen2,
