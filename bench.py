@@ -58,9 +58,9 @@ TRAFFIC_RECORDS = {
                            "paper_2608_21240_amd/csrc/tile_index.h",
                            "paper_2608_21240_amd/csrc/combine.hip",
                            "paper_2608_21240_amd/csrc/spice_internal.h"),
-        "source_sha256_16": "1bcd0063098c4d68",
-        "fetch_kib_per_call": 12028.2 + 184121.3 + 90272.0 + 905.6,
-        "write_kib_per_call": 260.2 + 675.8 + 1195.7 + 128.0,
+        "source_sha256_16": "e8a26807e663b9b1",
+        "fetch_kib_per_call": 12027.7 + 184120.7 + 90271.6 + 905.8,
+        "write_kib_per_call": 260.1 + 675.8 + 1195.7 + 128.0,
         "fetch_factor": 2.0,
         "write_factor": 1.0,
         "profile": "profiles/layer_dsv2_decode_kernel_trace_counters.md",
@@ -75,8 +75,8 @@ TRAFFIC_RECORDS = {
                            "paper_2608_21240_amd/csrc/tile_index.h",
                            "paper_2608_21240_amd/csrc/combine.hip",
                            "paper_2608_21240_amd/csrc/spice_internal.h"),
-        "source_sha256_16": "1bcd0063098c4d68",
-        "fetch_kib_per_call": 12020.6 + 55303.7 + 26301.8 + 903.1,
+        "source_sha256_16": "e8a26807e663b9b1",
+        "fetch_kib_per_call": 12020.2 + 55299.8 + 26300.5 + 903.2,
         "write_kib_per_call": 260.0 + 675.8 + 1195.9 + 128.0,
         "fetch_factor": 2.0,
         "write_factor": 1.0,
@@ -88,8 +88,8 @@ TRAFFIC_RECORDS = {
                            "paper_2608_21240_amd/csrc/expert_ffn_tiles.h",
                            "paper_2608_21240_amd/csrc/tile_index.h",
                            "paper_2608_21240_amd/csrc/spice_internal.h"),
-        "source_sha256_16": "acdfee8cac4f802c",
-        "fetch_kib_per_call": 189111.6 + 96772.1,
+        "source_sha256_16": "465506b906ed4aec",
+        "fetch_kib_per_call": 189111.4 + 96782.2,
         "write_kib_per_call": 462.4 + 1452.0,
         "fetch_factor": 2.0,
         "write_factor": 1.0,
@@ -102,8 +102,8 @@ TRAFFIC_RECORDS = {
                            "paper_2608_21240_amd/csrc/expert_ffn_tiles.h",
                            "paper_2608_21240_amd/csrc/tile_index.h",
                            "paper_2608_21240_amd/csrc/spice_internal.h"),
-        "source_sha256_16": "509691984fdb0f6c",
-        "fetch_kib_per_call": 60290.1 + 32779.9,
+        "source_sha256_16": "80a39a6da44636e1",
+        "fetch_kib_per_call": 60285.5 + 32778.9,
         "write_kib_per_call": 462.6 + 1452.0,
         "fetch_factor": 2.0,
         "write_factor": 1.0,
